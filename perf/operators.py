@@ -289,7 +289,7 @@ def _own(state):
     workspace = U.alloc_head_workspace(p, h.device)
     if c["op"] == "scores_grad":
         o = U.token_scores(p, h, w, state["targets"], workspace=workspace)
-        d_hidden, d_W = U.token_scores_bwd(p, h, w, state["targets"], o.lse, o.entropy, state["d_logp"], state["d_entropy"],
+        d_hidden, d_W = U.token_scores_bwd(p, h, w, state["targets"], o, state["d_logp"], state["d_entropy"],
                                            workspace=workspace)
         return dict(logp=o.logp, entropy=o.entropy, d_hidden=d_hidden, d_W=d_W)
     o = U.distill_fwd(p, h, w, state["teacher_ids"], state["teacher_logp"], state["weights"], workspace=workspace)
