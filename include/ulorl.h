@@ -331,6 +331,112 @@ int ulorl_token_loss_step_host(const ulorl_params_t* params,
                                float* h_loss, void* h_stats, void* h_d_hidden, void* h_d_W,
                                void* d_arena, size_t arena_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------ token scores and distillation
+ *
+ * The LM head beyond the policy loss: log-probabilities of given tokens with entropy and the most likely
+ * alternatives (what a rollout records as old_logp, what a reference policy hands over as ref_logp, what a teacher
+ * hands to a student), the gradients of a caller's own loss on log-probabilities and entropies, and distillation
+ * from a teacher's top logits.  All calls follow the conventions above: caller-owned device memory, no
+ * synchronisation, device findings in the workspace status word, bit-identical results for equal inputs.  With
+ *     a[t, v] = hidden[t] . W[v],  z = inv_temperature a,  p = softmax(z[t, :]),  lse = ln sum_v e^z
+ * hidden [T,H], W [V,H] have the type `dtype`; the T x V logits are never written to global memory (CUDA-core
+ * path: beyond one token panel of float32).  Any T >= 0; H a multiple of 8.
+ */
+typedef enum { ULORL_F16 = 2 } ulorl_logits_dtype_t;      /* further type of ulorl_logits_scores                   */
+
+/* What a teacher's list l[t, k] of log-probabilities at ids[t, k] means.
+ *   RAW     q_k = e^l_k: part of the teacher's distribution; what is not listed is left out of the loss
+ *   RENORM  q = softmax(teacher_inv_temperature l) over the list (l may be raw logits)
+ *   TAIL    q_k = e^l_k, and the remainder 1 - sum q is one more event, set against the student's
+ *           probability of everything that is not listed                                                           */
+typedef enum { ULORL_DISTILL_RAW = 0, ULORL_DISTILL_RENORM = 1, ULORL_DISTILL_TAIL = 2 } ulorl_distill_mode_t;
+
+#define ULORL_MAX_TOP 32      /* alternatives per token of the scoring calls                                       */
+#define ULORL_MAX_LIST 128    /* entries per token of a teacher's list                                             */
+
+typedef struct {
+  int32_t T, H, V;             /* packed tokens, hidden size, vocabulary                                           */
+  int32_t dtype;               /* ulorl_dtype_t of hidden, W, d_hidden                                             */
+  int32_t top_k;               /* scores: alternatives returned per token (0 .. ULORL_MAX_TOP, at most V);         */
+                               /* distillation: entries per token of the teacher's list (1 .. ULORL_MAX_LIST)      */
+  int32_t kernel_path;         /* AUTO, SIMT or TENSOR                                                             */
+  float inv_temperature;       /* kappa multiplying the logits                                                     */
+  int32_t bwd_panel_tokens;    /* backward: tokens per staging panel; 0 = library default                          */
+  int32_t dw_accumulate;       /* backward: 0 overwrite d_W, 1 add into it                                         */
+  int32_t dw_dtype;            /* ulorl_dtype_t of d_W                                                             */
+  int32_t distill_mode;        /* ulorl_distill_mode_t                                                             */
+  float teacher_inv_temperature; /* RENORM only; 1 in the other modes                                              */
+  int64_t norm_tokens;         /* distillation: N of the loss; 0 means T                                           */
+} ulorl_head_params_t;
+
+/* Bytes of workspace of the calls below (pure host function; 0 on invalid params).  backward = 0: enough for
+ * ulorl_token_scores and ulorl_distill_fwd; 1: for the backward calls as well.  Nothing in the workspace has to
+ * survive from one call to the next. */
+size_t ulorl_head_workspace_bytes(const ulorl_head_params_t* params, int32_t backward);
+
+/*
+ * Scores of T tokens.  targets [T] int32 may be NULL (then logp must be NULL).  Outputs, each optional:
+ *   logp[T] = z[t, y_t] - lse_t, entropy[T] = -sum p ln p, lse[T], norm[T][2] = (max_v a, ln sum_v e^(z - max z)),
+ *   eight-byte aligned: the softmax in a form that keeps 1 - p of sharply peaked rows, read by ulorl_token_scores_bwd;
+ *   top_ids[T][top_k] int32 and top_logp[T][top_k]: the largest entries of the row in falling order, equal ones by
+ *   rising id (both or neither; with top_k = 0 both NULL).  A row with fewer than top_k comparable logits (NaN
+ *   among them) has id -1 and a NaN there.
+ * A target outside [0, V) is reported in the status word and clamped.
+ */
+int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, const void* W, const int32_t* targets,
+                       float* logp, float* entropy, float* lse, float* norm, int32_t* top_ids, float* top_logp,
+                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Gradients of a loss with d loss / d logp_t = d_logp[t] and d loss / d entropy_t = d_entropy[t] (either may be NULL
+ * = zero, not both):
+ *   dz[t, v] = kappa (d_logp (1[v = y_t] - p_v) - d_entropy p_v (ln p_v + entropy)),
+ *   d_hidden = dz W (params->dtype), d_W = dz^T hidden (params->dw_dtype, added into when params->dw_accumulate).
+ * norm, logp and entropy are the outputs of ulorl_token_scores (logp and targets are read with d_logp, entropy with
+ * d_entropy).  A row whose two gradients are zero adds nothing, whatever its softmax; its hidden state must be
+ * finite all the same.
+ */
+int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
+                           const int32_t* targets, const float* norm, const float* logp, const float* entropy,
+                           const float* d_logp, const float* d_entropy, void* d_hidden, void* d_W,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The same scores for a caller that holds logits [T][ld] (a decoding step about to sample): dtype F32, BF16 or F16,
+ * V valid columns, ld >= V elements between rows, any alignment.  Entries of -inf (a grammar's or a sampler's mask)
+ * have probability zero; they come last among the alternatives, by rising id.  A row without any other entry has
+ * lse = logp = top_logp = -inf and entropy 0.  A target outside [0, V) gets logp NaN (there is no workspace whose
+ * status word could tell).  One kernel launch, no workspace; runs in [0, T) x [0, V) only, so padding columns may
+ * hold anything.
+ */
+int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V, int64_t ld, int32_t top_k,
+                        float inv_temperature, const int32_t* targets, float* logp, float* entropy, float* lse,
+                        int32_t* top_ids, float* top_logp, void* cuda_stream);
+
+/*
+ * Distillation from a teacher's top logits, top_k entries per token: teacher_ids [T][top_k] int32 in any order, -1 =
+ * no entry; teacher_logp [T][top_k] f32; weights [T] f32 or NULL (= 1).  With q as the mode says, Q = sum_k q_k and
+ * P the student's probability of the listed ids:
+ *   kl_t = sum_k q_k (ln q_k - ln p[ids_k])  (+ (1 - Q)(ln(1 - Q) - ln(1 - P)) in mode TAIL; 0 for an empty list)
+ *   loss = 1/N sum_t weights_t kl_t
+ * An id that is listed twice is two entries of one event: its probabilities add in the gradient.  An id outside
+ * [-1, V) is reported in the status word and left out.  Outputs: loss[1], kl[T], lse[T] (optional), and for the
+ * backward call norm[T][2], coef[T] (d loss / d z_v = coef p_v off the list) and entry_grad[T][top_k] (d loss / d z at
+ * the entry's id).
+ */
+int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
+                      const int32_t* teacher_ids, const float* teacher_logp, const float* weights,
+                      float* loss, float* kl, float* lse, float* norm, float* coef, float* entry_grad,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Its gradients: d_hidden [T,H] (params->dtype) and d_W [V,H] (params->dw_dtype, added into when
+ * params->dw_accumulate), times grad_loss (device scalar, NULL = 1).  A token of weight 0 or with an empty list adds
+ * nothing; its hidden state must be finite all the same. */
+int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
+                      const int32_t* teacher_ids, const float* norm, const float* coef, const float* entry_grad,
+                      const float* grad_loss, void* d_hidden, void* d_W,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

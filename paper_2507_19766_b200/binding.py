@@ -50,6 +50,15 @@ class CParams(ctypes.Structure):
     ]
 
 
+class CHeadParams(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("top_k", ctypes.c_int32), ("kernel_path", ctypes.c_int32), ("inv_temperature", ctypes.c_float),
+        ("bwd_panel_tokens", ctypes.c_int32), ("dw_accumulate", ctypes.c_int32), ("dw_dtype", ctypes.c_int32),
+        ("distill_mode", ctypes.c_int32), ("teacher_inv_temperature", ctypes.c_float), ("norm_tokens", ctypes.c_int64),
+    ]
+
+
 class CStats(ctypes.Structure):
     _fields_ = [
         ("loss", ctypes.c_float), ("mean_entropy", ctypes.c_float),
@@ -66,7 +75,9 @@ EXPORTS = ("ulorl_workspace_bytes", "ulorl_token_loss_fwd", "ulorl_token_loss_de
            "ulorl_check_status", "ulorl_status_string", "ulorl_launch_count", "ulorl_kernel_timing_begin",
            "ulorl_kernel_timing_end", "ulorl_host_step_arena_bytes", "ulorl_token_loss_step_host",
            "ulorl_token_loss_decide_static", "ulorl_group_advantages", "ulorl_sequence_entropy_partials",
-           "ulorl_sequence_entropy_combine", "ulorl_decision_thresholds", "ulorl_selftest_bounded_wait")
+           "ulorl_sequence_entropy_combine", "ulorl_decision_thresholds", "ulorl_selftest_bounded_wait",
+           "ulorl_head_workspace_bytes", "ulorl_token_scores", "ulorl_token_scores_bwd", "ulorl_logits_scores",
+           "ulorl_distill_fwd", "ulorl_distill_bwd")
 STATIC_MAX_TOKENS, STATIC_MAX_SEQS = 1 << 20, 1 << 16
 KERNEL_KINDS = ("stats", "dz", "d_hidden", "d_W")
 
@@ -121,6 +132,20 @@ def load_library() -> ctypes.CDLL:
     lib.ulorl_host_step_arena_bytes.argtypes = [cp]
     lib.ulorl_token_loss_step_host.restype = ctypes.c_int
     lib.ulorl_token_loss_step_host.argtypes = [cp] + [vp] * 17 + [vp, ctypes.c_size_t, vp]
+    hp = ctypes.POINTER(CHeadParams)
+    lib.ulorl_head_workspace_bytes.restype = ctypes.c_size_t
+    lib.ulorl_head_workspace_bytes.argtypes = [hp, ctypes.c_int32]
+    lib.ulorl_token_scores.restype = ctypes.c_int
+    lib.ulorl_token_scores.argtypes = [hp] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
+    lib.ulorl_token_scores_bwd.restype = ctypes.c_int
+    lib.ulorl_token_scores_bwd.argtypes = [hp] + [vp] * 10 + [vp, ctypes.c_size_t, vp]
+    lib.ulorl_logits_scores.restype = ctypes.c_int
+    lib.ulorl_logits_scores.argtypes = ([vp] + [ctypes.c_int32] * 3 + [ctypes.c_int64, ctypes.c_int32, ctypes.c_float] +
+                                        [vp] * 7)
+    lib.ulorl_distill_fwd.restype = ctypes.c_int
+    lib.ulorl_distill_fwd.argtypes = [hp] + [vp] * 11 + [vp, ctypes.c_size_t, vp]
+    lib.ulorl_distill_bwd.restype = ctypes.c_int
+    lib.ulorl_distill_bwd.argtypes = [hp] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
     _lib = lib
     return lib
 

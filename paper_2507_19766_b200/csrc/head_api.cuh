@@ -1,0 +1,562 @@
+// Host side of token scoring and distillation (included by ulorl_api.cu): validation, workspace, launches.
+#pragma once
+
+#include "scores.cuh"
+
+namespace ulorl {
+
+constexpr int kHeadMaxSplits = 128;        // merge_scores_kernel walks up to four lists a lane
+
+struct HeadPlan {
+  bool tensor;
+  int sms, workers;                        // workers: CTA pairs
+  int n_split, tiles_per_split;            // vocabulary splits of the forward sweep
+  int panel_tokens, n_panels;
+  size_t dz_ld;
+  bool dw_direct;                          // d_W leaves the contraction as bf16: one panel, nothing to add to
+  bool dw_acc;                             // d_W summed in float32 in the workspace, rounded at the end
+  int dh_parts, dh_part_blocks, dh_part_rows;
+  // forward scratch
+  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_sorted, off_slots, off_list_z, fwd_total;
+  // backward scratch, over the same bytes
+  size_t off_row_p, off_row_ins, off_panel, off_dw_acc, off_parts, bwd_total;
+};
+
+static bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
+static int validate_head(const ulorl_head_params_t* p) {
+  if (!p) return ULORL_ERR_INVALID_ARG;
+  if (p->T < 0 || p->H <= 0 || p->V <= 0 || p->top_k < 0) return ULORL_ERR_INVALID_ARG;
+  if (p->dtype != ULORL_F32 && p->dtype != ULORL_BF16) return ULORL_ERR_UNSUPPORTED;
+  if (p->dw_dtype != ULORL_F32 && p->dw_dtype != ULORL_BF16) return ULORL_ERR_INVALID_ARG;
+  if (p->kernel_path < ULORL_PATH_AUTO || p->kernel_path > ULORL_PATH_TENSOR_1CTA) return ULORL_ERR_INVALID_ARG;
+  if (p->kernel_path == ULORL_PATH_TENSOR_1CTA) return ULORL_ERR_UNSUPPORTED;
+  if (p->kernel_path == ULORL_PATH_TENSOR && p->dtype != ULORL_BF16) return ULORL_ERR_UNSUPPORTED;
+  if (!(p->inv_temperature > 0.f) || !std::isfinite(p->inv_temperature)) return ULORL_ERR_INVALID_ARG;
+  if (!(p->teacher_inv_temperature > 0.f) || !std::isfinite(p->teacher_inv_temperature)) return ULORL_ERR_INVALID_ARG;
+  if (p->distill_mode < ULORL_DISTILL_RAW || p->distill_mode > ULORL_DISTILL_TAIL) return ULORL_ERR_INVALID_ARG;
+  if (p->distill_mode != ULORL_DISTILL_RENORM && p->teacher_inv_temperature != 1.f) return ULORL_ERR_INVALID_ARG;
+  if (p->norm_tokens < 0 || p->bwd_panel_tokens < 0) return ULORL_ERR_INVALID_ARG;
+  if (p->dw_accumulate != 0 && p->dw_accumulate != 1) return ULORL_ERR_INVALID_ARG;
+  if (p->top_k > ULORL_MAX_LIST) return ULORL_ERR_UNSUPPORTED;
+  if (p->H % 8 != 0) return ULORL_ERR_UNSUPPORTED;
+  return ULORL_OK;
+}
+
+static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
+  HeadPlan pl{};
+  pl.tensor = p->dtype == ULORL_BF16 && p->kernel_path != ULORL_PATH_SIMT;
+  pl.sms = device_sm_count();
+  pl.workers = std::max(1, pl.sms / 2);
+  const int T = p->T, V = p->V, H = p->H;
+  const size_t T1 = (size_t)std::max(T, 1), K = (size_t)p->top_k;
+  const int tile_m = 2 * kBM;
+  const int m_tiles = std::max(1, (T + tile_m - 1) / tile_m);
+  const int n_tiles = (V + kBN - 1) / kBN;
+  pl.n_split = 1;
+  pl.tiles_per_split = n_tiles;
+  if (pl.tensor) {
+    // As for the policy loss: as few splits as keep the live hidden tiles in L2, then the best wave quantisation
+    // among the next few.  Unlike there the splits of a small batch go up to the worker count, so that every
+    // SM streams its share of W.
+    int want = (8 * pl.workers + m_tiles - 1) / m_tiles;
+    want = std::min(want, pl.workers);
+    const size_t live_bytes = (size_t)pl.workers * (size_t)tile_m * (size_t)H * 2;
+    const int fit = (int)((live_bytes + kStatsHiddenBudget - 1) / kStatsHiddenBudget);
+    want = std::max(1, std::min(std::max(want, fit), std::min(kHeadMaxSplits, n_tiles)));
+    auto cost_of = [&](int s) {
+      const int tps = (n_tiles + s - 1) / s;
+      const int s_eff = (n_tiles + tps - 1) / tps;
+      const long waves = ((long)m_tiles * s_eff + pl.workers - 1) / pl.workers;
+      return waves * tps;
+    };
+    const int s_max = std::min(std::min(want + 3, kHeadMaxSplits), n_tiles);
+    long best = cost_of(want);
+    for (int s = want + 1; s <= s_max; ++s) best = std::min(best, cost_of(s));
+    for (int s = want; s <= s_max; ++s)
+      if (cost_of(s) * 100 <= best * 101) { want = s; break; }
+    pl.tiles_per_split = (n_tiles + want - 1) / want;
+    pl.n_split = (n_tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
+  }
+  // backward panels
+  int panel = p->bwd_panel_tokens > 0 ? p->bwd_panel_tokens : (pl.tensor ? pl.workers * tile_m : kDefaultPanelSimt);
+  if (!pl.tensor) panel = std::min(panel, 32768);                   // rows are a grid dimension there
+  const int unit = pl.tensor ? tile_m : kSimtTile;
+  panel = (int)std::min<long>((long)align_up((size_t)panel, (size_t)unit), (long)align_up(T1, (size_t)unit));
+  pl.panel_tokens = panel;
+  pl.n_panels = (int)((T1 + panel - 1) / panel);
+  pl.dz_ld = pl.tensor ? align_up((size_t)V, 64) : (size_t)V;
+  const bool want_bf16 = p->dw_dtype == ULORL_BF16;
+  pl.dw_direct = pl.tensor && want_bf16 && pl.n_panels == 1 && !p->dw_accumulate;
+  pl.dw_acc = want_bf16 && !pl.dw_direct;
+  // d_hidden: few token tiles make few units (256 x 512 outputs each), so the vocabulary is cut into parts until
+  // the units fill the GPU; the parts are float32 and added in order
+  pl.dh_parts = 1;
+  if (pl.tensor) {
+    const int k_blocks = (V + kBK - 1) / kBK;
+    const int units = ((panel + tile_m - 1) / tile_m) * ((H + 2 * kBN - 1) / (2 * kBN));
+    int parts = units >= pl.workers ? 1 : pl.workers / units;
+    parts = std::max(1, std::min(parts, k_blocks / 16));            // a part keeps at least 1024 vocabulary entries
+    pl.dh_part_blocks = (k_blocks + parts - 1) / parts;
+    pl.dh_parts = (k_blocks + pl.dh_part_blocks - 1) / pl.dh_part_blocks;
+    pl.dh_part_rows = (int)align_up((size_t)panel, (size_t)tile_m);
+  }
+  size_t off = 256;
+  pl.off_status = 0;
+  pl.off_partials = off;  off = align_up(off + sizeof(float4) * (size_t)pl.n_split * T1, 256);
+  pl.off_acc_y = off;     off = align_up(off + sizeof(float) * T1, 256);
+  pl.off_top_val = off;   off = align_up(off + sizeof(float) * (size_t)pl.n_split * T1 * K, 256);
+  pl.off_top_id = off;    off = align_up(off + sizeof(int) * (size_t)pl.n_split * T1 * K, 256);
+  pl.off_sorted = off;    off = align_up(off + sizeof(int) * T1 * K, 256);
+  pl.off_list_z = off;    off = align_up(off + sizeof(float) * T1 * K, 256);
+  pl.off_slots = off;     off = align_up(off + T1 * K, 1024);
+  pl.off_panel = off;     // the CUDA-core path's forward pass holds a panel of logits
+  pl.fwd_total = pl.tensor ? off : align_up(off + sizeof(float) * (size_t)panel * pl.dz_ld, 1024);
+  off = 256;
+  pl.off_row_p = off;     off = align_up(off + sizeof(float4) * T1, 256);
+  pl.off_row_ins = off;   off = align_up(off + sizeof(float) * T1, 1024);
+  if (pl.tensor) pl.off_panel = off;
+  else off = pl.off_panel = std::max(off, pl.off_panel);
+  off = align_up(off + (size_t)panel * pl.dz_ld * (pl.tensor ? 2 : 4), 1024);
+  if (pl.dw_acc) { pl.off_dw_acc = off; off = align_up(off + sizeof(float) * (size_t)V * (size_t)H, 1024); }
+  if (pl.dh_parts > 1) {
+    pl.off_parts = off;
+    off = align_up(off + sizeof(float) * (size_t)pl.dh_parts * (size_t)pl.dh_part_rows * (size_t)H, 1024);
+  }
+  pl.bwd_total = std::max(off, pl.fwd_total);
+  return pl;
+}
+
+template <int kMode>
+static int launch_pair(const HeadPlan& pl, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc,
+                       const UmmaArgs& a, cudaStream_t stream) {
+  return launch_umma_impl<kMode, 2, acc_per_unit_pair<kMode>()>(ma, mb, mc, a, pl.sms, stream);
+}
+
+// The forward sweep of hidden against W on the tensor cores; `a` carries the mode's own fields.
+static int run_sweep(const ulorl_head_params_t* p, const HeadPlan& pl, int mode, UmmaArgs a, const void* hidden,
+                     const void* W, uint8_t* ws, cudaStream_t stream) {
+  CUtensorMap map_a, map_b;
+  int st = make_map_bf16(&map_a, hidden, (uint64_t)p->T, (uint64_t)p->H, (uint64_t)p->H, kBK, kBM);
+  if (st != ULORL_OK) return st;
+  st = make_map_bf16(&map_b, W, (uint64_t)p->V, (uint64_t)p->H, (uint64_t)p->H, kBK, kBN / 2);
+  if (st != ULORL_OK) return st;
+  a.M = p->T; a.N = p->V; a.K = p->H;
+  a.m_tiles = (p->T + 2 * kBM - 1) / (2 * kBM);
+  a.n_tiles = (p->V + kBN - 1) / kBN;
+  a.n_split = pl.n_split;
+  a.split_stride = a.tiles_per_split = pl.tiles_per_split;
+  a.kappa = p->inv_temperature;
+  a.partials = reinterpret_cast<float4*>(ws + pl.off_partials);
+  a.T_total = p->T;
+  a.status = reinterpret_cast<int*>(ws + pl.off_status);
+  switch (mode) {
+    case kModeScores: return launch_pair<kModeScores>(pl, map_a, map_b, map_a, a, stream);
+    case kModeScoresTop8: return launch_pair<kModeScoresTop8>(pl, map_a, map_b, map_a, a, stream);
+    case kModeScoresTop32: return launch_pair<kModeScoresTop32>(pl, map_a, map_b, map_a, a, stream);
+    default: return launch_pair<kModeDistill>(pl, map_a, map_b, map_a, a, stream);
+  }
+}
+
+// panel[i, v] = hidden[t0 + i] . W[v] in float32 on CUDA cores.
+template <typename TIn>
+static int simt_logits_panel(const ulorl_head_params_t* p, const void* hidden, const void* W, int t0, int rows, float* panel,
+                             size_t ld, cudaStream_t stream) {
+  const dim3 grid((p->V + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
+  simt_gemm_kernel<TIn, TIn, float><<<grid, kSimtThreads, 0, stream>>>(
+      static_cast<const TIn*>(hidden) + (size_t)t0 * p->H, (size_t)p->H, 1, static_cast<const TIn*>(W), 1, (size_t)p->H,
+      panel, ld, rows, p->V, p->H, 0);
+  return check_launch();
+}
+
+template <typename T>
+static int launch_rows(const RowsArgs& a, cudaStream_t stream) {
+  logits_rows_kernel<T><<<a.T, kRowThreads, 0, stream>>>(a);
+  return check_launch();
+}
+
+static int head_begin(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, void* workspace,
+                      size_t workspace_bytes, size_t need, cudaStream_t stream) {
+  if (!hidden || !W || !workspace) return ULORL_ERR_INVALID_ARG;
+  if (!aligned16(hidden) || !aligned16(W) || !aligned16(workspace)) return ULORL_ERR_UNSUPPORTED;
+  if (workspace_bytes < need) return ULORL_ERR_WORKSPACE;
+  (void)p;
+  if (cudaMemsetAsync(static_cast<uint8_t*>(workspace) + pl.off_status, 0, 256, stream) != cudaSuccess) return ULORL_ERR_CUDA;
+  return ULORL_OK;
+}
+
+// dz panels and the two gradient contractions.  row_p (and row_ins, targets) say what a row of dz is; put_list
+// writes the teacher lists' columns of a panel, if there are any.
+static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W,
+                        const int32_t* targets, const float4* row_p, const float* row_ins,
+                        const std::function<int(int, int)>& put_list, void* d_hidden, void* d_W_out, uint8_t* ws,
+                        cudaStream_t stream) {
+  const int T = p->T, H = p->H, V = p->V;
+  float* d_W = pl.dw_acc ? reinterpret_cast<float*>(ws + pl.off_dw_acc) : static_cast<float*>(d_W_out);
+  const int acc_into = pl.dw_acc ? 0 : p->dw_accumulate;
+  int st;
+  if (pl.tensor) {
+    __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + pl.off_panel);
+    const int tile_m = 2 * kBM;
+    CUtensorMap map_hidden_k, map_w_k, map_w_mn, map_hidden_mn, map_dw, map_parts;
+    st = make_map_bf16(&map_hidden_k, hidden, (uint64_t)T, (uint64_t)H, (uint64_t)H, kBK, kBM);
+    if (st != ULORL_OK) return st;
+    st = make_map_bf16(&map_w_k, W, (uint64_t)V, (uint64_t)H, (uint64_t)H, kBK, kBN / 2);
+    if (st != ULORL_OK) return st;
+    st = make_map_bf16(&map_w_mn, W, (uint64_t)V, (uint64_t)H, (uint64_t)H, 64, kBK);
+    if (st != ULORL_OK) return st;
+    st = make_map_bf16(&map_hidden_mn, hidden, (uint64_t)T, (uint64_t)H, (uint64_t)H, 64, kBK);
+    if (st != ULORL_OK) return st;
+    st = pl.dw_direct ? make_map_bf16(&map_dw, d_W_out, (uint64_t)V, (uint64_t)H, (uint64_t)H, 64, kBM)
+                      : make_map(&map_dw, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, d_W, (uint64_t)V, (uint64_t)H, (uint64_t)H, 32, kBM);
+    if (st != ULORL_OK) return st;
+    float* parts = reinterpret_cast<float*>(ws + pl.off_parts);
+    if (pl.dh_parts > 1) {
+      st = make_map(&map_parts, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, parts, (uint64_t)pl.dh_parts * pl.dh_part_rows, (uint64_t)H,
+                    (uint64_t)H, 32, kBM);
+      if (st != ULORL_OK) return st;
+    }
+    const int h_tiles = (H + 2 * kBN - 1) / (2 * kBN);
+    for (int t0 = 0, panel = 0; t0 < T; t0 += pl.panel_tokens, ++panel) {
+      const int rows = std::min(T - t0, pl.panel_tokens);
+      CUtensorMap dz_out, dz_k, dz_mn;
+      st = make_map_bf16(&dz_out, dz, (uint64_t)pl.panel_tokens, (uint64_t)pl.dz_ld, (uint64_t)pl.dz_ld, 64, kBM);
+      if (st != ULORL_OK) return st;
+      st = make_map_bf16(&dz_k, dz, (uint64_t)rows, (uint64_t)pl.dz_ld, (uint64_t)pl.dz_ld, kBK, kBM);
+      if (st != ULORL_OK) return st;
+      st = make_map_bf16(&dz_mn, dz, (uint64_t)rows, (uint64_t)pl.dz_ld, (uint64_t)pl.dz_ld, 64, kBK);
+      if (st != ULORL_OK) return st;
+      UmmaArgs a{};
+      a.M = rows; a.N = V; a.K = H;
+      a.m_tiles = (rows + tile_m - 1) / tile_m;
+      a.n_tiles = (int)((pl.dz_ld + kBN - 1) / kBN);
+      a.group_m = kRasterGroup;
+      a.a_mn0 = a.row0 = t0;
+      a.kappa = p->inv_temperature;
+      a.targets = targets;
+      a.row_p = row_p;
+      a.row_ins = row_ins;
+      a.dz_cols = (int)pl.dz_ld;
+      a.status = reinterpret_cast<int*>(ws + pl.off_status);
+      st = launch_pair<kModeDzRow>(pl, map_hidden_k, map_w_k, dz_out, a, stream);
+      if (st != ULORL_OK) return st;
+      if (put_list) {
+        st = put_list(t0, rows);
+        if (st != ULORL_OK) return st;
+      }
+      // d_hidden[t0 + m, h] = sum_v dz[m, v] W[v, h]
+      UmmaArgs b{};
+      b.M = rows; b.N = H; b.K = V;
+      b.m_tiles = (rows + tile_m - 1) / tile_m;
+      b.n_tiles = h_tiles;
+      b.group_m = kGradRasterGroup;
+      b.row0 = t0;
+      b.out_ld = (size_t)H;
+      b.status = a.status;
+      if (pl.dh_parts > 1) {
+        b.n_split = pl.dh_parts;
+        b.part_blocks = pl.dh_part_blocks;
+        b.part_rows = pl.dh_part_rows;
+        st = launch_pair<kModeDHiddenPart>(pl, dz_k, map_w_mn, map_parts, b, stream);
+        if (st != ULORL_OK) return st;
+        const size_t n = (size_t)rows * (size_t)H;
+        sum_parts_kernel<<<(unsigned)((n / 8 + 255) / 256), 256, 0, stream>>>(
+            parts, pl.dh_parts, (size_t)pl.dh_part_rows * (size_t)H, n, static_cast<__nv_bfloat16*>(d_hidden) + (size_t)t0 * H);
+        ULORL_LAUNCH_CHECK();
+      } else {
+        b.d_hidden = static_cast<__nv_bfloat16*>(d_hidden);
+        st = launch_pair<kModeDHidden>(pl, dz_k, map_w_mn, map_w_mn, b, stream);
+        if (st != ULORL_OK) return st;
+      }
+      // d_W[v, h] (+)= sum_m dz[m, v] hidden[t0 + m, h]
+      UmmaArgs c{};
+      c.M = V; c.N = H; c.K = rows;
+      c.m_tiles = (V + tile_m - 1) / tile_m;
+      c.n_tiles = h_tiles;
+      c.group_m = kGradRasterGroup;
+      c.b_k0 = t0;
+      c.d_W = d_W;
+      c.out_ld = (size_t)H;
+      c.dz_cols = H;
+      c.accumulate = (panel > 0 || acc_into) ? 1 : 0;
+      c.status = a.status;
+      st = pl.dw_direct ? launch_pair<kModeDWBf16>(pl, dz_mn, map_hidden_mn, map_dw, c, stream)
+                        : launch_pair<kModeDW>(pl, dz_mn, map_hidden_mn, map_dw, c, stream);
+      if (st != ULORL_OK) return st;
+    }
+  } else {
+    float* dz = reinterpret_cast<float*>(ws + pl.off_panel);
+    const size_t ld = pl.dz_ld;
+    for (int t0 = 0, panel = 0; t0 < T; t0 += pl.panel_tokens, ++panel) {
+      const int rows = std::min(T - t0, pl.panel_tokens);
+      const int acc = (panel > 0 || acc_into) ? 1 : 0;
+      const dim3 gdz((unsigned)std::min((V + 1023) / 1024, 64), rows);
+      const dim3 gdh((H + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
+      const dim3 gdw((H + kSimtTile - 1) / kSimtTile, (V + kSimtTile - 1) / kSimtTile);
+      const bool f32 = p->dtype == ULORL_F32;
+      st = f32 ? simt_logits_panel<float>(p, hidden, W, t0, rows, dz, ld, stream)
+               : simt_logits_panel<__nv_bfloat16>(p, hidden, W, t0, rows, dz, ld, stream);
+      if (st != ULORL_OK) return st;
+      dz_rows_f32_kernel<<<gdz, 256, 0, stream>>>(dz, ld, V, t0, p->inv_temperature, row_p, row_ins, targets);
+      ULORL_LAUNCH_CHECK();
+      if (put_list) {
+        st = put_list(t0, rows);
+        if (st != ULORL_OK) return st;
+      }
+      if (f32) {
+        simt_gemm_kernel<float, float, float><<<gdh, kSimtThreads, 0, stream>>>(
+            dz, ld, 1, static_cast<const float*>(W), (size_t)H, 1, static_cast<float*>(d_hidden) + (size_t)t0 * H, (size_t)H,
+            rows, H, V, 0);
+        ULORL_LAUNCH_CHECK();
+        simt_gemm_kernel<float, float, float><<<gdw, kSimtThreads, 0, stream>>>(
+            dz, 1, ld, static_cast<const float*>(hidden) + (size_t)t0 * H, (size_t)H, 1, d_W, (size_t)H, V, H, rows, acc);
+        ULORL_LAUNCH_CHECK();
+      } else {
+        simt_gemm_kernel<float, __nv_bfloat16, __nv_bfloat16><<<gdh, kSimtThreads, 0, stream>>>(
+            dz, ld, 1, static_cast<const __nv_bfloat16*>(W), (size_t)H, 1,
+            static_cast<__nv_bfloat16*>(d_hidden) + (size_t)t0 * H, (size_t)H, rows, H, V, 0);
+        ULORL_LAUNCH_CHECK();
+        simt_gemm_kernel<float, __nv_bfloat16, float><<<gdw, kSimtThreads, 0, stream>>>(
+            dz, 1, ld, static_cast<const __nv_bfloat16*>(hidden) + (size_t)t0 * H, (size_t)H, 1, d_W, (size_t)H, V, H, rows, acc);
+        ULORL_LAUNCH_CHECK();
+      }
+    }
+  }
+  if (pl.dw_acc) return round_dw_rows(d_W, d_W_out, 0, V, H, p->dw_accumulate, stream);
+  return ULORL_OK;
+}
+
+// T == 0: the gradient of nothing.
+static int empty_head_bwd(const ulorl_head_params_t* p, void* d_W, cudaStream_t stream) {
+  if (!d_W) return ULORL_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)p->V * (size_t)p->H * (p->dw_dtype == ULORL_BF16 ? 2 : 4);
+  if (!p->dw_accumulate && cudaMemsetAsync(d_W, 0, bytes, stream) != cudaSuccess) return ULORL_ERR_CUDA;
+  return ULORL_OK;
+}
+
+}  // namespace ulorl
+
+extern "C" {
+
+size_t ulorl_head_workspace_bytes(const ulorl_head_params_t* params, int32_t backward) {
+  if (validate_head(params) != ULORL_OK) return 0;
+  const HeadPlan pl = make_head_plan(params);
+  return backward ? pl.bwd_total : pl.fwd_total;
+}
+
+int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, const void* W, const int32_t* targets,
+                       float* logp, float* entropy, float* lse, float* norm, int32_t* top_ids, float* top_logp,
+                       void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  TraceRange trace("ulorl token scores");
+  int st = validate_head(params);
+  if (st != ULORL_OK) return st;
+  const int T = params->T, V = params->V, k = params->top_k;
+  if (k > ULORL_MAX_TOP) return ULORL_ERR_UNSUPPORTED;
+  if (k > V) return ULORL_ERR_INVALID_ARG;
+  if (T == 0) return ULORL_OK;
+  if ((k > 0) != (top_ids != nullptr) || (k > 0) != (top_logp != nullptr)) return ULORL_ERR_INVALID_ARG;
+  if (logp && !targets) return ULORL_ERR_INVALID_ARG;
+  if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const HeadPlan pl = make_head_plan(params);
+  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.fwd_total, stream);
+  if (st != ULORL_OK) return st;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (pl.tensor) {
+    UmmaArgs a{};
+    a.targets = logp ? targets : nullptr;
+    a.acc_y = reinterpret_cast<float*>(ws + pl.off_acc_y);
+    a.top_k = k;
+    a.top_val = reinterpret_cast<float*>(ws + pl.off_top_val);
+    a.top_id = reinterpret_cast<int*>(ws + pl.off_top_id);
+    st = run_sweep(params, pl, k == 0 ? kModeScores : (k <= 8 ? kModeScoresTop8 : kModeScoresTop32), a, hidden, W, ws, stream);
+    if (st != ULORL_OK) return st;
+    MergeArgs m{};
+    m.T = T; m.n_split = pl.n_split; m.k = k;
+    m.kappa = params->inv_temperature;
+    m.partials = reinterpret_cast<const float4*>(ws + pl.off_partials);
+    m.acc_y = a.acc_y;
+    m.top_val = a.top_val; m.top_id = a.top_id;
+    m.logp = logp; m.entropy = entropy; m.lse = lse;
+    m.norm = reinterpret_cast<float2*>(norm);
+    m.out_ids = top_ids; m.out_logp = top_logp;
+    const size_t per_warp = sizeof(unsigned long long) * (size_t)pl.n_split * (size_t)k;   // at most 32 KB
+    int warps = 8;
+    while (warps > 1 && per_warp * warps > 48u * 1024u) warps /= 2;
+    merge_scores_kernel<<<(T + warps - 1) / warps, warps * 32, per_warp * warps, stream>>>(m);
+    return check_launch();
+  }
+  float* panel = reinterpret_cast<float*>(ws + pl.off_panel);
+  for (int t0 = 0; t0 < T; t0 += pl.panel_tokens) {
+    const int rows = std::min(T - t0, pl.panel_tokens);
+    st = params->dtype == ULORL_F32 ? simt_logits_panel<float>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream)
+                                    : simt_logits_panel<__nv_bfloat16>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream);
+    if (st != ULORL_OK) return st;
+    RowsArgs a{};
+    a.logits = panel; a.ld = pl.dz_ld;
+    a.T = rows; a.V = V; a.k = k;
+    a.kappa = params->inv_temperature;
+    a.targets = targets ? targets + t0 : nullptr;
+    a.logp = logp ? logp + t0 : nullptr;
+    a.entropy = entropy ? entropy + t0 : nullptr;
+    a.lse = lse ? lse + t0 : nullptr;
+    a.norm = norm ? reinterpret_cast<float2*>(norm) + t0 : nullptr;
+    a.top_ids = top_ids ? top_ids + (size_t)t0 * k : nullptr;
+    a.top_logp = top_logp ? top_logp + (size_t)t0 * k : nullptr;
+    a.status = reinterpret_cast<int*>(ws + pl.off_status);
+    st = launch_rows<float>(a, stream);
+    if (st != ULORL_OK) return st;
+  }
+  return ULORL_OK;
+}
+
+int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
+                           const int32_t* targets, const float* norm, const float* logp, const float* entropy,
+                           const float* d_logp, const float* d_entropy, void* d_hidden, void* d_W,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  TraceRange trace("ulorl token scores backward");
+  int st = validate_head(params);
+  if (st != ULORL_OK) return st;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const int T = params->T;
+  if (T == 0) return empty_head_bwd(params, d_W, stream);
+  if (!norm || !d_hidden || !d_W || (!d_logp && !d_entropy)) return ULORL_ERR_INVALID_ARG;
+  if ((d_logp && (!logp || !targets)) || (d_entropy && !entropy)) return ULORL_ERR_INVALID_ARG;
+  if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
+  const HeadPlan pl = make_head_plan(params);
+  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.bwd_total, stream);
+  if (st != ULORL_OK) return st;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  float4* row_p = reinterpret_cast<float4*>(ws + pl.off_row_p);
+  float* row_ins = reinterpret_cast<float*>(ws + pl.off_row_ins);
+  row_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<const float2*>(norm), logp,
+                                                         entropy, d_logp, d_entropy, row_p, row_ins);
+  ULORL_LAUNCH_CHECK();
+  return run_head_bwd(params, pl, hidden, W, d_logp ? targets : nullptr, row_p, row_ins, nullptr, d_hidden, d_W, ws, stream);
+}
+
+int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V, int64_t ld, int32_t top_k,
+                        float inv_temperature, const int32_t* targets, float* logp, float* entropy, float* lse,
+                        int32_t* top_ids, float* top_logp, void* cuda_stream) {
+  TraceRange trace("ulorl logits scores");
+  if (T < 0 || V <= 0 || ld < V || top_k < 0 || top_k > V) return ULORL_ERR_INVALID_ARG;
+  if (dtype != ULORL_F32 && dtype != ULORL_BF16 && dtype != ULORL_F16) return ULORL_ERR_UNSUPPORTED;
+  if (top_k > ULORL_MAX_TOP) return ULORL_ERR_UNSUPPORTED;
+  if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature)) return ULORL_ERR_INVALID_ARG;
+  if (T == 0) return ULORL_OK;
+  if ((top_k > 0) != (top_ids != nullptr) || (top_k > 0) != (top_logp != nullptr)) return ULORL_ERR_INVALID_ARG;
+  if (logp && !targets) return ULORL_ERR_INVALID_ARG;
+  if (!logits || (reinterpret_cast<uintptr_t>(logits) & (dtype == ULORL_F32 ? 3u : 1u))) return ULORL_ERR_INVALID_ARG;
+  RowsArgs a{};
+  a.logits = logits; a.ld = (size_t)ld;
+  a.T = T; a.V = V; a.k = top_k;
+  a.kappa = inv_temperature;
+  a.targets = targets;
+  a.logp = logp; a.entropy = entropy; a.lse = lse;
+  a.top_ids = top_ids; a.top_logp = top_logp;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  return dtype == ULORL_F32 ? launch_rows<float>(a, stream)
+                            : (dtype == ULORL_BF16 ? launch_rows<__nv_bfloat16>(a, stream) : launch_rows<__half>(a, stream));
+}
+
+int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
+                      const int32_t* teacher_ids, const float* teacher_logp, const float* weights,
+                      float* loss, float* kl, float* lse, float* norm, float* coef, float* entry_grad,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  TraceRange trace("ulorl distillation");
+  int st = validate_head(params);
+  if (st != ULORL_OK) return st;
+  const int T = params->T, V = params->V, K = params->top_k;
+  if (K < 1 || !loss) return ULORL_ERR_INVALID_ARG;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (T == 0) return cudaMemsetAsync(loss, 0, sizeof(float), stream) == cudaSuccess ? ULORL_OK : ULORL_ERR_CUDA;
+  if (!teacher_ids || !teacher_logp || !kl || !norm || !coef || !entry_grad) return ULORL_ERR_INVALID_ARG;
+  if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
+  const HeadPlan pl = make_head_plan(params);
+  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.fwd_total, stream);
+  if (st != ULORL_OK) return st;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  int* status = reinterpret_cast<int*>(ws + pl.off_status);
+  int* sorted = reinterpret_cast<int*>(ws + pl.off_sorted);
+  uint8_t* slots = ws + pl.off_slots;
+  float* list_z = reinterpret_cast<float*>(ws + pl.off_list_z);
+  float4* partials = reinterpret_cast<float4*>(ws + pl.off_partials);
+  const unsigned row_blocks = (unsigned)((T + 7) / 8);              // eight warps, one token each
+  distill_sort_kernel<<<row_blocks, 256, 0, stream>>>(T, K, V, teacher_ids, sorted, slots, status);
+  ULORL_LAUNCH_CHECK();
+  if (pl.tensor) {
+    UmmaArgs a{};
+    a.list_k = K;
+    a.list_ids = sorted;
+    a.list_z = list_z;
+    st = run_sweep(params, pl, kModeDistill, a, hidden, W, ws, stream);
+    if (st != ULORL_OK) return st;
+  } else {
+    float* panel = reinterpret_cast<float*>(ws + pl.off_panel);
+    for (int t0 = 0; t0 < T; t0 += pl.panel_tokens) {
+      const int rows = std::min(T - t0, pl.panel_tokens);
+      st = params->dtype == ULORL_F32 ? simt_logits_panel<float>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream)
+                                      : simt_logits_panel<__nv_bfloat16>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream);
+      if (st != ULORL_OK) return st;
+      distill_take_kernel<<<(rows + 7) / 8, 256, 0, stream>>>(rows, t0, K, panel, pl.dz_ld, sorted, list_z);
+      ULORL_LAUNCH_CHECK();
+      RowsArgs a{};
+      a.logits = panel; a.ld = pl.dz_ld;
+      a.T = rows; a.V = V;
+      a.kappa = params->inv_temperature;
+      a.partials = partials + t0;
+      st = launch_rows<float>(a, stream);
+      if (st != ULORL_OK) return st;
+    }
+  }
+  DistillRowArgs d{};
+  d.T = T; d.K = K; d.n_split = pl.n_split; d.mode = params->distill_mode;
+  d.kappa = params->inv_temperature;
+  d.teacher_kappa = params->teacher_inv_temperature;
+  d.inv_N = 1.0 / (params->norm_tokens > 0 ? (double)params->norm_tokens : (double)T);
+  d.partials = partials;
+  d.list_z = list_z; d.slots = slots;
+  d.teacher = teacher_logp; d.weights = weights;
+  d.kl = kl; d.norm = reinterpret_cast<float2*>(norm); d.lse = lse; d.coef = coef; d.entry_grad = entry_grad;
+  distill_rows_kernel<<<row_blocks, 256, 0, stream>>>(d);
+  ULORL_LAUNCH_CHECK();
+  distill_loss_kernel<<<1, 1024, 0, stream>>>(T, kl, weights, d.inv_N, loss);
+  return check_launch();
+}
+
+int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
+                      const int32_t* teacher_ids, const float* norm, const float* coef, const float* entry_grad,
+                      const float* grad_loss, void* d_hidden, void* d_W,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  TraceRange trace("ulorl distillation backward");
+  int st = validate_head(params);
+  if (st != ULORL_OK) return st;
+  const int T = params->T, V = params->V, K = params->top_k;
+  if (K < 1) return ULORL_ERR_INVALID_ARG;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (T == 0) return empty_head_bwd(params, d_W, stream);
+  if (!teacher_ids || !norm || !coef || !entry_grad || !d_hidden || !d_W) return ULORL_ERR_INVALID_ARG;
+  if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
+  const HeadPlan pl = make_head_plan(params);
+  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.bwd_total, stream);
+  if (st != ULORL_OK) return st;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  float4* row_p = reinterpret_cast<float4*>(ws + pl.off_row_p);
+  distill_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<const float2*>(norm),
+                                                             coef, grad_loss, row_p);
+  ULORL_LAUNCH_CHECK();
+  auto put_list = [&](int t0, int rows) -> int {
+    const size_t n = (size_t)rows * (size_t)K;
+    const unsigned blocks = (unsigned)((n + 255) / 256);
+    if (pl.tensor)
+      distill_put_kernel<<<blocks, 256, 0, stream>>>(rows, t0, K, V, params->inv_temperature, grad_loss, teacher_ids, entry_grad,
+                                                     reinterpret_cast<__nv_bfloat16*>(ws + pl.off_panel), pl.dz_ld);
+    else
+      distill_put_kernel<<<blocks, 256, 0, stream>>>(rows, t0, K, V, params->inv_temperature, grad_loss, teacher_ids, entry_grad,
+                                                     reinterpret_cast<float*>(ws + pl.off_panel), pl.dz_ld);
+    return check_launch();
+  };
+  return run_head_bwd(params, pl, hidden, W, nullptr, row_p, nullptr, put_list, d_hidden, d_W, ws, stream);
+}
+
+}  // extern "C"

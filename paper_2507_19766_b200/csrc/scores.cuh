@@ -1,0 +1,791 @@
+// Kernels of token scoring and of distillation from a teacher's top logits, around the contractions:
+// logits_rows_kernel   softmax statistics, log-prob, entropy and the k largest entries of rows of logits
+// merge_scores_kernel  the same from the partials of the LM-head sweep
+// distill_*_kernel     teacher lists: sorting, the loss of a row, its gradient on the list, the batch loss
+// row_params_kernel    what the dz pass of a row needs
+//
+// A row's softmax is kept as (m, r): m the maximum of the raw logits a, r the sum of e^(kappa (a - m)) over all
+// entries but one that equals m, so that 1 - p and the entropy keep their relative precision in sharply peaked rows;
+// ln s = log1p(r), lse = kappa m + ln s.  Ids are chosen by (value falling, id rising).
+#pragma once
+
+#include <cuda_fp16.h>
+#include <limits.h>
+
+#include "common.cuh"
+#include "simt.cuh"
+
+namespace ulorl {
+
+constexpr int kMaxTop = 32;            // alternatives a scoring call returns
+constexpr int kMaxList = 128;          // entries of a teacher's list
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float fast_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// max that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// Unsigned keys in the order of the values: -inf < ... < -0 = +0 < ... < +inf, NaN below them all (0).
+__device__ __forceinline__ uint32_t order_key(float x) {
+  if (x != x) return 0u;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  if (k == 0u) return __uint_as_float(0x7FC00000u);
+  return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
+}
+constexpr uint32_t kKeyNegInf = 0x007FFFFFu;
+
+__device__ __forceinline__ unsigned long long pack_entry(uint32_t key, int id) {
+  return ((unsigned long long)key << 32) | (uint32_t)~id;          // larger = better: value, then the lower id
+}
+
+template <typename T> struct RowType;
+template <> struct RowType<float> { static constexpr int per_vec = 4, key_bits = 32; };
+template <> struct RowType<__nv_bfloat16> { static constexpr int per_vec = 8, key_bits = 16; };
+template <> struct RowType<__half> { static constexpr int per_vec = 8, key_bits = 19; };   // 8 exponent + 10 mantissa bits + sign
+
+__device__ __forceinline__ void widen(const uint4& v, float (&x)[4], float) {
+  x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ void widen(const uint4& v, float (&x)[8], __nv_bfloat16) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void widen(const uint4& v, float (&x)[8], __half) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+__device__ __forceinline__ float row_value(float x) { return x; }
+__device__ __forceinline__ float row_value(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float row_value(__half x) { return __half2float(x); }
+
+struct RowsArgs {
+  const void* logits;       // [T][ld], V valid columns
+  size_t ld;
+  int T, V, k;
+  float kappa;
+  const int* targets;       // may be NULL
+  float *logp, *entropy, *lse;
+  float2* norm;             // (m, ln s)
+  int* top_ids;             // [T][k]
+  float* top_logp;          // [T][k]
+  float4* partials;         // (m, r, -, -) for a merge that follows
+  int* status;              // NULL: a target out of range gets a NaN
+};
+
+constexpr int kRowThreads = 256;
+constexpr int kRowUnroll = 4;          // 16-byte loads a thread has in flight
+constexpr int kRowCandidates = 512;
+
+// Running statistics of a row in one lane: m is the warp's maximum, s and u are the lane's sums over its entries
+// relative to m (u in units of log2) without one entry that equals m where own = 1.
+struct RowState {
+  float m = -INFINITY, s = 0.f, u = 0.f, own = 0.f;
+  float lane_max = NAN;                                             // no entry yet
+
+  // folds in n entries (absent ones are -inf; `any`: the lane has some); all lanes of a warp together
+  template <int n>
+  __device__ __forceinline__ void fold(const float (&x)[n], float c2, bool any) {
+    float cmax = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < n; ++j) cmax = fmaxf(cmax, x[j]);
+    if (any) lane_max = fmaxf(lane_max, cmax);
+    float wmax = cmax;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) wmax = fmaxf(wmax, __shfl_xor_sync(0xffffffffu, wmax, o));
+    float ls = 0.f, lu = 0.f;
+    if (wmax > m) {                                                 // the same in all lanes
+      if (m > -INFINITY) {
+        const float d = fmaxf((m - wmax) * c2, -1000.f), sc = fast_ex2(d);   // m may be the type's lowest value
+        u = sc * fmaf(d, s + own, u);
+        s = (s + own) * sc;
+        own = 0.f;
+      }
+      m = wmax;
+      float ties = 0.f;
+#pragma unroll
+      for (int j = 0; j < n; ++j) {
+        const float t = max_nan((x[j] - m) * c2, -1000.f);          // an entry of -inf: 0 * -1000, not 0 * -inf
+        const float e = fast_ex2(t);
+        const bool top = x[j] == m;
+        ties += top ? 1.f : 0.f;
+        ls += top ? 0.f : e;
+        lu = fmaf(e, t, lu);
+      }
+      if (ties > 0.f) { own = 1.f; ls += ties - 1.f; }
+    } else {
+      const float ref = m > -INFINITY ? m : 0.f;
+#pragma unroll
+      for (int j = 0; j < n; ++j) {
+        const float t = max_nan((x[j] - ref) * c2, -1000.f);
+        const float e = fast_ex2(t);
+        ls += e;
+        lu = fmaf(e, t, lu);
+      }
+    }
+    s += ls;
+    u += lu;
+  }
+};
+
+// One block per row, one pass over memory: each warp keeps a running maximum for its lanes, each lane its sums
+// relative to it, and its own largest entry.  The k-th largest of the 256 lane maxima bounds the k-th largest
+// entry from below, and entries at or above it sit in lanes whose maximum is: only their few vectors are read again.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads)
+logits_rows_kernel(const RowsArgs args) {
+  constexpr int E = RowType<T>::per_vec;
+  constexpr int kShift = 32 - RowType<T>::key_bits;
+  __shared__ float sh_m[kRowThreads / 32], sh_s[kRowThreads / 32], sh_u[kRowThreads / 32];
+  __shared__ int sh_n[kRowThreads / 32];
+  __shared__ float sh_row[2];                                       // m, ln s
+  __shared__ unsigned long long cand[kRowCandidates];
+  __shared__ int owners[kRowThreads];
+  __shared__ int n_owner, n_cand, sh_scan[kRowThreads / 32 + 1];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int V = args.V, k = args.k;
+  const int row = blockIdx.x;
+  const T* base = static_cast<const T*>(args.logits) + (size_t)row * args.ld;
+  // [0, head) and [V - tail, V) are read element by element, the vectors between them start on 16 bytes
+  const int head = min(V, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(base) & 15u)) & 15u) / sizeof(T)));
+  const int nvec = (V - head) / E;
+  const int extras = V - nvec * E;                                  // head + tail < 2 E
+  const uint4* vecs = reinterpret_cast<const uint4*>(base + head);
+  auto extra_id = [&](int i) { return i < head ? i : nvec * E + i; };
+  const float c2 = args.kappa * kLog2e;
+
+  RowState st;
+
+  {
+    float x[1] = {-INFINITY};
+    if (tid < extras) x[0] = row_value(base[extra_id(tid)]);
+    st.fold<1>(x, c2, tid < extras);
+  }
+  for (int b = 0; b < nvec; b += kRowUnroll * kRowThreads) {
+    uint4 v[kRowUnroll] = {};
+    float x[kRowUnroll * E];
+#pragma unroll
+    for (int q = 0; q < kRowUnroll; ++q) {
+      const int i = b + q * kRowThreads + tid;
+      if (i < nvec) v[q] = __ldg(vecs + i);
+    }
+#pragma unroll
+    for (int q = 0; q < kRowUnroll; ++q) {
+      const int i = b + q * kRowThreads + tid;
+      float w[E];
+      widen(v[q], w, T());
+#pragma unroll
+      for (int j = 0; j < E; ++j) x[q * E + j] = i < nvec ? w[j] : -INFINITY;
+    }
+    st.fold<kRowUnroll * E>(x, c2, b + tid < nvec);
+  }
+
+  // ---- merge lanes, then warps
+  {
+    float s = st.s, u = st.u, n = st.own;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      u += __shfl_xor_sync(0xffffffffu, u, o);
+      n += __shfl_xor_sync(0xffffffffu, n, o);
+    }
+    if (lane == 0) { sh_m[warp] = st.m; sh_s[warp] = s; sh_u[warp] = u; sh_n[warp] = (int)n; }
+  }
+  if (tid == 0) { n_owner = 0; n_cand = 0; }
+  __syncthreads();
+  if (tid == 0) {
+    float M = -INFINITY;
+    for (int w = 0; w < kRowThreads / 32; ++w) M = fmaxf(M, sh_m[w]);
+    float r = 0.f, uu = 0.f;
+    int at_max = 0;
+    for (int w = 0; w < kRowThreads / 32; ++w) {
+      if (sh_m[w] == M) {
+        r += sh_s[w];
+        uu += sh_u[w];
+        at_max += sh_n[w];
+      } else {
+        const float tot = sh_s[w] + (float)sh_n[w];
+        if (sh_m[w] > -INFINITY) {
+          const float d = fmaxf((sh_m[w] - M) * c2, -1000.f), sc = fast_ex2(d);
+          r = fmaf(tot, sc, r);
+          uu = fmaf(sc, fmaf(d, tot, sh_u[w]), uu);
+        } else {
+          r += sh_s[w];                                             // nothing, or the NaN that a NaN entry left
+        }
+      }
+    }
+    if (at_max > 1) r += (float)(at_max - 1);
+    const bool nothing = M == -INFINITY && r == 0.f;                // no entry has a probability
+    const float ln_s = nothing ? 0.f : (M == -INFINITY ? __uint_as_float(0x7FC00000u) : log1pf(r));
+    sh_row[0] = M;
+    sh_row[1] = ln_s;
+    if (args.partials) args.partials[row] = make_float4(M, r, 0.f, 0.f);
+    if (args.lse) args.lse[row] = nothing ? -INFINITY : fmaf(args.kappa, M, ln_s);
+    if (args.norm) args.norm[row] = make_float2(M, ln_s);
+    if (args.entropy) args.entropy[row] = nothing ? 0.f : max_nan(ln_s - kLn2 * uu / (1.f + r), 0.f);
+    if (args.logp) {
+      int y = args.targets[row];
+      const bool bad = y < 0 || y >= V;
+      if (bad && args.status) {                                     // the LM-head calls report and clamp
+        atomicOr(args.status, kStatusBadTarget);
+        y = y < 0 ? 0 : V - 1;
+      }
+      args.logp[row] = bad && !args.status ? __uint_as_float(0x7FC00000u)
+                       : nothing           ? -INFINITY
+                                           : args.kappa * (row_value(base[y]) - M) - ln_s;
+    }
+  }
+  if (k == 0) return;
+
+  // ---- the k largest
+  const bool holds = tid < nvec || tid < extras;
+  const uint32_t mine = holds ? (order_key(st.lane_max) >> kShift) : 0u;
+  uint32_t tau = 0u;                                                // largest class with at least k lane maxima in or above it
+#pragma unroll 1
+  for (int bit = 31 - kShift; bit >= 0; --bit) {
+    const uint32_t c = tau | (1u << bit);
+    if (__syncthreads_count(mine >= c) >= k) tau = c;
+  }
+  tau = max(tau, 1u);                                               // 0 is NaN's class
+  if (mine >= tau) owners[atomicAdd(&n_owner, 1)] = tid;
+  __syncthreads();
+  const int per_lane = (nvec + kRowThreads - 1) / kRowThreads;
+  auto offer = [&](float x, int id, uint32_t least) {
+    const uint32_t key = order_key(x);
+    if ((key >> kShift) >= least) {
+      const int at = atomicAdd(&n_cand, 1);
+      if (at < kRowCandidates) cand[at] = pack_entry(key, id);
+    }
+  };
+  // entries of class `least` or above, from the lanes whose maximum is
+  auto collect = [&](uint32_t least) {
+    if (tid < extras && mine >= least) offer(row_value(base[extra_id(tid)]), extra_id(tid), least);
+    const int items = n_owner * per_lane;
+    for (int w = tid; w < items; w += kRowThreads) {
+      const int i = (w % per_lane) * kRowThreads + owners[w / per_lane];
+      if (i >= nvec) continue;
+      float x[E];
+      widen(__ldg(vecs + i), x, T());
+#pragma unroll
+      for (int j = 0; j < E; ++j) offer(x[j], head + i * E + j, least);
+    }
+    __syncthreads();
+  };
+  bool done = false;
+  // many lanes tie at tau, or tau is the masked entries' -inf: only what is above it is collected that way
+  const bool many = n_owner > 4 * k + 32 || tau <= (kKeyNegInf >> kShift);
+  if (!many) {
+    collect(tau);
+    done = n_cand >= k && n_cand <= kRowCandidates;
+  }
+  if (!done) {
+    __syncthreads();
+    if (tid == 0) { n_cand = 0; n_owner = 0; }
+    __syncthreads();
+    if (mine > tau) owners[atomicAdd(&n_owner, 1)] = tid;
+    __syncthreads();
+    collect(tau + 1u);
+    if (n_cand <= kRowCandidates - k) {
+      // then entries of tau's class in the order of their ids until there are k.  A class is one value: what a
+      // 16-bit type's key drops is constant
+      int have = n_cand;
+      for (int b = 0; b < V && have < k; b += kRowThreads) {
+        const int id = b + tid;
+        uint32_t key = 0u;
+        if (id < V) key = order_key(row_value(base[id]));
+        const bool hit = id < V && (key >> kShift) == tau;
+        const uint32_t votes = __ballot_sync(0xffffffffu, hit);
+        if (lane == 0) sh_scan[warp] = __popc(votes);
+        __syncthreads();
+        int before = 0, total = 0;
+        for (int w = 0; w < kRowThreads / 32; ++w) {
+          if (w < warp) before += sh_scan[w];
+          total += sh_scan[w];
+        }
+        const int at = have + before + __popc(votes & ((1u << lane) - 1u));
+        if (hit && at < k) cand[at] = pack_entry(key, id);
+        have = min(k, have + total);
+        __syncthreads();
+      }
+      if (tid == 0) n_cand = max(have, n_cand);
+      done = true;
+      __syncthreads();
+    }
+  }
+  const float M = sh_row[0], ln_s = sh_row[1];
+  auto put = [&](int at, unsigned long long entry) {
+    const float x = key_value((uint32_t)(entry >> 32));
+    args.top_ids[(size_t)row * k + at] = entry == 0ull ? -1 : (int)~(uint32_t)entry;
+    args.top_logp[(size_t)row * k + at] = M == -INFINITY && ln_s == 0.f ? (entry == 0ull ? x : -INFINITY)
+                                                                        : args.kappa * (x - M) - ln_s;
+  };
+  if (done) {
+    const int n = n_cand;
+    for (int c = tid; c < max(n, k); c += kRowThreads) {
+      if (c >= n) { put(c, 0ull); continue; }                       // fewer than k entries are numbers
+      const unsigned long long e = cand[c];
+      int rank = 0;
+      for (int o = 0; o < n; ++o) rank += cand[o] > e ? 1 : 0;
+      if (rank < k) put(rank, e);
+    }
+    return;
+  }
+  // a few lanes hold hundreds of entries above the bound: k passes, each for the best entry below the last one
+  unsigned long long last = ~0ull;
+  for (int at = 0; at < k; ++at) {
+    unsigned long long best = 0ull;
+    for (int id = tid; id < V; id += kRowThreads) {
+      const uint32_t key = order_key(row_value(base[id]));
+      const unsigned long long e = key ? pack_entry(key, id) : 0ull;
+      if (e < last && e > best) best = e;
+    }
+    __syncthreads();
+    cand[tid] = best;
+    __syncthreads();
+    for (int o = kRowThreads / 2; o > 0; o >>= 1) {
+      if (tid < o && cand[tid + o] > cand[tid]) cand[tid] = cand[tid + o];
+      __syncthreads();
+    }
+    last = cand[0];
+    if (tid == 0) put(at, last);
+    if (last == 0ull) {
+      for (int c = at + 1 + tid; c < k; c += kRowThreads) put(c, 0ull);
+      return;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Merge of the LM-head sweep's partials: one warp per token.  partials[split][t] = (m, r, u, -) as the sweep's
+// epilogue defines them (u in units of log2).
+// ------------------------------------------------------------------------------------------
+struct MergeArgs {
+  int T, n_split, k;
+  float kappa;
+  const float4* partials;
+  const float* acc_y;
+  const float* top_val;     // [n_split][T][k]
+  const int* top_id;
+  float *logp, *entropy, *lse;
+  float2* norm;
+  int* out_ids;             // [T][k]
+  float* out_logp;
+};
+
+// (m, r) of all splits of token t, in every lane of the warp; u likewise.
+__device__ __forceinline__ void merge_partials(const float4* __restrict__ partials, int n_split, int T, int t, float c2,
+                                               float& M, float& r, float& u) {
+  const int lane = threadIdx.x & 31;
+  M = -INFINITY;
+  for (int k = lane; k < n_split; k += 32) M = fmaxf(M, partials[(size_t)k * T + t].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  r = 0.f;
+  u = 0.f;
+  int at_max = 0;
+  for (int k = lane; k < n_split; k += 32) {
+    const float4 p = partials[(size_t)k * T + t];
+    if (p.x == M) {
+      if (M > -INFINITY) ++at_max;
+      r += p.y;
+      u += p.z;
+    } else if (p.x > -INFINITY) {
+      const float d = fmaxf((p.x - M) * c2, -1000.f), sc = fast_ex2(d);
+      r = fmaf(p.y + 1.f, sc, r);
+      u = fmaf(sc, fmaf(d, p.y + 1.f, p.z), u);
+    } else {
+      r += p.y;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    r += __shfl_xor_sync(0xffffffffu, r, o);
+    u += __shfl_xor_sync(0xffffffffu, u, o);
+    at_max += __shfl_xor_sync(0xffffffffu, at_max, o);
+  }
+  if (at_max > 1) r += (float)(at_max - 1);
+}
+
+__global__ void merge_scores_kernel(const MergeArgs a) {
+  extern __shared__ unsigned long long sh_lists[];                  // per warp [n_split * k]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int t = blockIdx.x * warps + warp;
+  if (t >= a.T) return;
+  float M, r, u;
+  merge_partials(a.partials, a.n_split, a.T, t, a.kappa * kLog2e, M, r, u);
+  const float ln_s = log1pf(r);
+  if (lane == 0) {
+    if (a.lse) a.lse[t] = fmaf(a.kappa, M, ln_s);
+    if (a.norm) a.norm[t] = make_float2(M, ln_s);
+    if (a.entropy) a.entropy[t] = max_nan(ln_s - kLn2 * u / (1.f + r), 0.f);
+    if (a.logp) a.logp[t] = a.kappa * (a.acc_y[t] - M) - ln_s;
+  }
+  if (a.k == 0) return;
+  // every split's list falls: lane l walks the lists of splits l, l + 32, ..., the warp takes the best head k times
+  unsigned long long* mine = sh_lists + (size_t)warp * a.n_split * a.k;
+  for (int i = lane; i < a.n_split * a.k; i += 32) {
+    const size_t at = ((size_t)(i / a.k) * a.T + t) * a.k + i % a.k;
+    const int id = a.top_id[at];
+    mine[i] = id < 0 ? 0ull : pack_entry(order_key(a.top_val[at]), id);
+  }
+  __syncwarp();
+  constexpr int kLists = 4;                                         // n_split <= 32 * kLists
+  int head[kLists];
+#pragma unroll
+  for (int q = 0; q < kLists; ++q) head[q] = 0;
+  for (int at = 0; at < a.k; ++at) {
+    unsigned long long best = 0ull;
+#pragma unroll
+    for (int q = 0; q < kLists; ++q) {
+      const int sp = lane + 32 * q;
+      if (sp < a.n_split && head[q] < a.k) {
+        const unsigned long long e = mine[sp * a.k + head[q]];
+        best = e > best ? e : best;
+      }
+    }
+    unsigned long long top = best;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
+      top = other > top ? other : top;
+    }
+    if (top != 0ull && best == top) {
+#pragma unroll
+      for (int q = 0; q < kLists; ++q) {
+        const int sp = lane + 32 * q;
+        if (sp < a.n_split && head[q] < a.k && mine[sp * a.k + head[q]] == top) ++head[q];
+      }
+    }
+    if (lane == 0) {
+      a.out_ids[(size_t)t * a.k + at] = top == 0ull ? -1 : (int)~(uint32_t)top;
+      a.out_logp[(size_t)t * a.k + at] = a.kappa * (key_value((uint32_t)(top >> 32)) - M) - ln_s;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------ gradients of scores
+// (m, log2 s, alpha, beta) and the value at the target's column for the dz pass:
+//   dz_j = kappa g (1[j = y] - p_j) - kappa e p_j (log p_j + H) = 2^L (alpha + beta L) off the target, L = log2 p_j.
+__global__ void row_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ logp,
+                                  const float* __restrict__ entropy, const float* __restrict__ d_logp,
+                                  const float* __restrict__ d_entropy, float4* __restrict__ row_p, float* __restrict__ row_ins) {
+  const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t >= T) return;
+  const float g = d_logp ? d_logp[t] : 0.f, e = d_entropy ? d_entropy[t] : 0.f;
+  const float H = d_entropy ? entropy[t] : 0.f;
+  const float2 n = norm[t];
+  row_p[t] = make_float4(n.x, n.y * kLog2e, -kappa * fmaf(e, H, g), -kappa * e * kLn2);
+  if (d_logp) {
+    const float l = logp[t];
+    row_ins[t] = kappa * (-expm1f(l) * g - (e != 0.f ? expf(l) * e * (l + H) : 0.f));
+  }
+}
+
+// dz of a panel of raw float32 logits in place (CUDA-core path): rows [t0, t0 + gridDim.y).
+__global__ void dz_rows_f32_kernel(float* __restrict__ panel, size_t ld, int V, int t0, float kappa,
+                                   const float4* __restrict__ row_p, const float* __restrict__ row_ins,
+                                   const int* __restrict__ targets) {
+  const int t = t0 + blockIdx.y;
+  float* row = panel + (size_t)blockIdx.y * ld;
+  const float4 rp = row_p[t];
+  const bool live = rp.z != 0.f || rp.w != 0.f;
+  int y = -1;
+  if (targets) y = min(max(targets[t], 0), V - 1);
+  const float c2 = kappa * kLog2e;
+  for (int v = blockIdx.x * blockDim.x + threadIdx.x; v < V; v += gridDim.x * blockDim.x) {
+    const float L = fmaf(row[v] - rp.x, c2, -rp.y);
+    float d = live ? exp2f(L) * fmaf(rp.w, L, rp.z) : 0.f;
+    if (v == y) d = row_ins[t];
+    row[v] = d;
+  }
+}
+
+// ------------------------------------------------------------------------------------------ distillation
+// Teacher lists, one warp per token: the distinct valid ids in rising order (then INT_MAX), and for every entry
+// the place of its id: bits 0-6, bit 7 set where an earlier entry has the same id; 255 for an entry that is padding
+// (-1) or out of range (reported).
+__global__ void distill_sort_kernel(int T, int K, int V, const int* __restrict__ ids, int* __restrict__ sorted,
+                                    uint8_t* __restrict__ slots, int* __restrict__ status) {
+  const int lane = threadIdx.x & 31;
+  const int t = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (t >= T) return;
+  constexpr int kPer = kMaxList / 32;
+  int id[kPer], rank[kPer];
+  bool first[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int i = q * 32 + lane;
+    id[q] = i < K ? ids[(size_t)t * K + i] : -1;
+    if (id[q] < -1 || id[q] >= V) {
+      atomicOr(status, kStatusBadTarget);
+      id[q] = -1;
+    }
+    first[q] = id[q] >= 0;
+    rank[q] = 0;
+  }
+#pragma unroll
+  for (int qj = 0; qj < kPer; ++qj) {
+    if (qj * 32 >= K) break;
+    for (int l = 0; l < 32; ++l) {
+      const int other = __shfl_sync(0xffffffffu, id[qj], l), j = qj * 32 + l;
+#pragma unroll
+      for (int q = 0; q < kPer; ++q)
+        if (other == id[q] && j < q * 32 + lane) first[q] = false;
+    }
+  }
+  int distinct = 0;
+#pragma unroll
+  for (int qj = 0; qj < kPer; ++qj) {
+    if (qj * 32 >= K) break;
+    const uint32_t firsts = __ballot_sync(0xffffffffu, first[qj]);
+    distinct += __popc(firsts);
+    for (int l = 0; l < 32; ++l) {
+      const int other = __shfl_sync(0xffffffffu, id[qj], l);
+      const bool counts = (firsts >> l) & 1u;
+#pragma unroll
+      for (int q = 0; q < kPer; ++q)
+        if (counts && other < id[q]) ++rank[q];
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int i = q * 32 + lane;
+    if (i >= K) break;
+    slots[(size_t)t * K + i] = id[q] < 0 ? 255u : (uint8_t)(rank[q] | (first[q] ? 0 : 128));
+    if (first[q]) sorted[(size_t)t * K + rank[q]] = id[q];
+    if (i >= distinct) sorted[(size_t)t * K + i] = INT_MAX;
+  }
+}
+
+// Float32 panel of raw logits: the list's logits are taken out (and replaced by -inf), one warp per token.
+__global__ void distill_take_kernel(int rows, int t0, int K, float* __restrict__ panel, size_t ld,
+                                    const int* __restrict__ sorted, float* __restrict__ list_z) {
+  const int lane = threadIdx.x & 31;
+  const int i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (i >= rows) return;
+  const size_t t = (size_t)t0 + i;
+  for (int q = lane; q < K; q += 32) {
+    const int id = sorted[t * K + q];
+    if (id == INT_MAX) continue;
+    list_z[t * K + q] = panel[(size_t)i * ld + id];
+    panel[(size_t)i * ld + id] = -INFINITY;
+  }
+}
+
+struct DistillRowArgs {
+  int T, K, n_split, mode;
+  float kappa, teacher_kappa;
+  double inv_N;
+  const float4* partials;   // (m, r, -, -) of the entries off the list, per split
+  const float* list_z;      // [T][K] raw logits by place
+  const uint8_t* slots;     // [T][K]
+  const float* teacher;     // [T][K]
+  const float* weights;     // [T] or NULL (1)
+  float* kl;                // [T]
+  float2* norm;             // [T] (m, ln s) over all entries
+  float* lse;               // [T] or NULL
+  float* coef;              // [T]: d loss / d z_j = coef p_j off the list
+  float* entry_grad;        // [T][K]: d loss / d z at the entry's id
+};
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ double warp_max(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// The loss of a token and its gradient on the list, one warp per token, in 64 bits: a token has at most 128 entries,
+// and 1 - sum q and the differences p - q cancel.
+__global__ void distill_rows_kernel(const DistillRowArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int t = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (t >= a.T) return;
+  constexpr int kPer = kMaxList / 32;
+  float m_off, r_off, unused;
+  merge_partials(a.partials, a.n_split, a.T, t, a.kappa * kLog2e, m_off, r_off, unused);
+  float z[kPer];
+  uint8_t slot[kPer];
+  double logq[kPer];
+  float top = m_off;
+  double tmax = -INFINITY;
+  int n_valid = 0, n_again = 0;
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int i = q * 32 + lane;
+    slot[q] = i < a.K ? a.slots[(size_t)t * a.K + i] : 255;
+    z[q] = -INFINITY;
+    logq[q] = -INFINITY;
+    if (slot[q] != 255) {
+      z[q] = a.list_z[(size_t)t * a.K + (slot[q] & 127)];
+      logq[q] = (double)a.teacher[(size_t)t * a.K + i] * a.teacher_kappa;
+      top = fmaxf(top, z[q]);
+      tmax = fmax(tmax, logq[q]);
+      ++n_valid;
+      n_again += slot[q] >> 7;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    n_valid += __shfl_xor_sync(0xffffffffu, n_valid, o);
+    n_again += __shfl_xor_sync(0xffffffffu, n_again, o);
+  }
+  const double kappa = (double)a.kappa;
+  // sum of e^(kappa (a - top)): off the list, then the list's distinct ids
+  const double rest = m_off > -INFINITY ? (1.0 + (double)r_off) * exp(kappa * ((double)m_off - (double)top)) : (double)r_off;
+  double on = 0.0;
+#pragma unroll
+  for (int q = 0; q < kPer; ++q)
+    if (slot[q] < 128) on += exp(kappa * ((double)z[q] - (double)top));
+  on = warp_sum(on);
+  const double ln_s = log(rest + on);
+  if (a.mode == ULORL_DISTILL_RENORM) {
+    tmax = warp_max(tmax);
+    const double shift = tmax > -INFINITY ? tmax : 0.0;
+    double sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) sum += exp(logq[q] - shift);
+    sum = log(warp_sum(sum)) + shift;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q)
+      if (tmax > -INFINITY) logq[q] -= sum;                         // a list without any probability stays without
+  }
+  double Q = 0.0, kl = 0.0, prob[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    prob[q] = 0.0;
+    if (slot[q] == 255) continue;
+    prob[q] = exp(logq[q]);
+    Q += prob[q];
+    if (prob[q] != 0.0) kl += prob[q] * (logq[q] - (kappa * ((double)z[q] - (double)top) - ln_s));
+  }
+  Q = warp_sum(Q);
+  kl = warp_sum(kl);
+  double c_on = Q, c_off = Q;
+  if (a.mode == ULORL_DISTILL_TAIL) {
+    const double rest_q = fmax(1.0 - Q, 0.0);
+    c_on = 1.0;
+    c_off = 1.0;
+    if (rest_q > 0.0) {
+      kl += rest_q * (log(rest_q) - (log(rest) - ln_s));
+      c_off = 1.0 - rest_q / (rest / (rest + on));
+    }
+  }
+  const double w = a.weights ? (double)a.weights[t] : 1.0;
+  const double scale = n_valid > 0 && w != 0.0 ? w * a.inv_N : 0.0;
+  if (lane == 0) {
+    a.kl[t] = n_valid > 0 ? (float)kl : 0.f;
+    a.norm[t] = make_float2(top, (float)ln_s);
+    if (a.lse) a.lse[t] = (float)(kappa * (double)top + ln_s);
+    a.coef[t] = scale != 0.0 && (m_off > -INFINITY) ? (float)(scale * c_off) : 0.f;
+  }
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int i = q * 32 + lane;
+    // an id that is listed again: its probabilities add, and every entry of it gets the whole gradient
+    double all = prob[q];
+    if (n_again > 0) {
+      all = 0.0;
+#pragma unroll
+      for (int qj = 0; qj < kPer; ++qj)
+        for (int l = 0; l < 32; ++l) {
+          const double p = __shfl_sync(0xffffffffu, prob[qj], l);
+          const int s = __shfl_sync(0xffffffffu, (int)slot[qj], l);
+          if (s != 255 && slot[q] != 255 && (s & 127) == (slot[q] & 127)) all += p;
+        }
+    }
+    if (i < a.K)
+      a.entry_grad[(size_t)t * a.K + i] =
+          slot[q] == 255 || scale == 0.0 ? 0.f
+                                         : (float)(scale * (c_on * exp(kappa * ((double)z[q] - (double)top) - ln_s) - all));
+  }
+}
+
+// loss = 1/N sum w_t kl_t, by one block in a fixed order.
+__global__ void distill_loss_kernel(int T, const float* __restrict__ kl, const float* __restrict__ weights, double inv_N,
+                                    float* __restrict__ loss) {
+  __shared__ double part[1024];
+  double acc = 0.0;
+  for (int t = threadIdx.x; t < T; t += 1024) {
+    const double w = weights ? (double)weights[t] : 1.0;
+    if (w != 0.0) acc += w * (double)kl[t];
+  }
+  part[threadIdx.x] = acc;
+  __syncthreads();
+  for (int o = 512; o > 0; o >>= 1) {
+    if (threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *loss = (float)(part[0] * inv_N);
+}
+
+// Row parameters of the dz pass: dz_j = kappa grad_loss coef p_j off the list.
+__global__ void distill_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ coef,
+                                      const float* __restrict__ grad_loss, float4* __restrict__ row_p) {
+  const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t >= T) return;
+  const float gl = grad_loss ? *grad_loss : 1.f;
+  row_p[t] = make_float4(norm[t].x, norm[t].y * kLog2e, kappa * gl * coef[t], 0.f);
+}
+
+// The list's columns of a dz panel: rows [t0, t0 + rows).  Entries of one id carry the same value.
+template <typename TDz>
+__global__ void distill_put_kernel(int rows, int t0, int K, int V, float kappa, const float* __restrict__ grad_loss,
+                                   const int* __restrict__ ids, const float* __restrict__ entry_grad,
+                                   TDz* __restrict__ panel, size_t ld) {
+  const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= (size_t)rows * K) return;
+  const size_t at = (size_t)t0 * K + i;
+  const int id = ids[at];
+  if (id < 0 || id >= V) return;
+  const float gl = grad_loss ? *grad_loss : 1.f;
+  from_f32(panel[(i / K) * ld + id], kappa * gl * entry_grad[at]);
+}
+
+// d_hidden of a panel from the parts over the vocabulary, added in the order of the parts.
+__global__ void sum_parts_kernel(const float* __restrict__ parts, int n_parts, size_t part_stride, size_t n,
+                                 __nv_bfloat16* __restrict__ out) {
+  const size_t i = ((size_t)blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  if (i >= n) return;                                               // n is a multiple of 8 (H is)
+  float acc[8] = {};
+  for (int p = 0; p < n_parts; ++p) {
+    const float4* src = reinterpret_cast<const float4*>(parts + (size_t)p * part_stride + i);
+    const float4 x = src[0], y = src[1];
+    acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
+    acc[4] += y.x; acc[5] += y.y; acc[6] += y.z; acc[7] += y.w;
+  }
+  uint32_t w[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(acc[2 * q], acc[2 * q + 1]);
+    w[q] = *reinterpret_cast<uint32_t*>(&h);
+  }
+  *reinterpret_cast<uint4*>(out + i) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+}  // namespace ulorl

@@ -296,22 +296,24 @@ static int launch_umma_impl(const CUtensorMap& ma, const CUtensorMap& mb, const 
       opted_in[dev] = true;
     }
   }
-  const int units = (kMode == kModeStats) ? a.m_tiles * a.n_split : a.m_tiles * a.n_tiles;
+  using Tr = ModeTraits<kMode>;
+  const int units = Tr::sweep ? a.m_tiles * a.n_split
+                              : a.m_tiles * a.n_tiles * (kMode == kModeDHiddenPart ? a.n_split : 1);
   if (units <= 0) return ULORL_OK;
-  if (kMode != kModeStats && a.group_m <= 0) return ULORL_ERR_INVALID_ARG;
+  if (!Tr::sweep && a.group_m <= 0) return ULORL_ERR_INVALID_ARG;
   // L2 policy of the tile loads: keep what is re-read for long (the hidden tile of the two logits
   // kernels, the slices of W / of the hidden panel that every pair sweeps in the gradient kernels).
   // The statistics kernel marks its W stream too: it starts in an L2 that the gradient kernels of the
   // step before left full of evict-last lines, which unmarked loads cannot displace.
   UmmaArgs a2 = a;
-  a2.l2_a = (kMode == kModeStats || kMode == kModeDz) ? ptx::kL2EvictLast : ptx::kL2Normal;
-  a2.l2_b = (kMode == kModeStats || kMode == kModeDHidden || kMode == kModeDW) ? ptx::kL2EvictLast : ptx::kL2Normal;
+  a2.l2_a = (Tr::sweep || Tr::dz) ? ptx::kL2EvictLast : ptx::kL2Normal;
+  a2.l2_b = (Tr::sweep || Tr::dh || Tr::dw) ? ptx::kL2EvictLast : ptx::kL2Normal;
   const int max_workers = num_sms / kCta;
   const int workers = units < max_workers ? units : max_workers;
   cudaEvent_t e0 = nullptr, e1 = nullptr;
   if (g_timing.enabled.load(std::memory_order_relaxed)) {
-    e0 = timing_event(kMode);
-    e1 = timing_event(kMode);
+    e0 = timing_event(Tr::timing_kind);
+    e1 = timing_event(Tr::timing_kind);
     if (e0 && e1) cudaEventRecord(e0, stream);
   }
   cudaLaunchConfig_t cfg{};
@@ -338,7 +340,7 @@ static int launch_umma_impl(const CUtensorMap& ma, const CUtensorMap& mb, const 
 
 // Accumulators per unit: the gradient contractions on CTA pairs use two (256 x 512 outputs a unit).
 template <int kMode>
-static constexpr int acc_per_unit_pair() { return (kMode == kModeDHidden || kMode == kModeDW) ? 2 : 1; }
+static constexpr int acc_per_unit_pair() { return (ModeTraits<kMode>::dh || ModeTraits<kMode>::dw) ? 2 : 1; }
 static int grad_unit_cols(const Plan& pl) { return pl.cta == 2 ? 2 * kBN : kBN; }
 
 // mc is the output tensor map of the dz and d_W kernels; the other kernels get any valid map and ignore it.
@@ -1346,3 +1348,5 @@ int ulorl_token_loss_step_host(const ulorl_params_t* params, const void* h_hidde
 }
 
 }  // extern "C"
+
+#include "head_api.cuh"

@@ -7,6 +7,16 @@
 //   kModeDHidden d_hidden[t, :] = sum_v dz[t, v] W[v, :]
 //   kModeDW      d_W[v, :] (+)= sum_t dz[t, v] hidden[t, :]
 //
+// and the variants of these that token scoring and distillation use:
+//
+//   kModeScores, kModeScoresTop8, kModeScoresTop32
+//                statistics as (max, sum without the maximum's own 1), with the 0, 8 or 32 largest logits of a
+//                row kept beside them in registers
+//   kModeDistill statistics of the entries that are not on the token's list; the logits of those that are go out
+//   kModeDzRow   dz = softmax * (alpha + beta log2 softmax) with per-row alpha and beta, one column overwritten
+//   kModeDHiddenPart  d_hidden over a part of the vocabulary, float32 (few token tiles: the parts fill the GPU)
+//   kModeDWBf16  d_W rounded to bf16 in the epilogue (all tokens in one launch)
+//
 // One kernel template umma_kernel<mode, CTAs per MMA, accumulators per unit>, persistent, one CTA per
 // SM, 192 threads: one thread of warp 0 feeds a shared-memory ring with TMA tile loads (128-byte
 // swizzle), one thread of warp 1 issues tcgen05.mma into tensor memory, warps 2-5 drain accumulators
@@ -20,6 +30,8 @@
 // gradient contractions, dz in the d_W one) are loaded as MN-major tiles; nothing is transposed in
 // global memory.  No TMA multicast is used.  Every mbarrier wait is bounded.
 #pragma once
+
+#include <limits.h>
 
 #include "common.cuh"
 #include "ptx_sm100.cuh"
@@ -50,8 +62,27 @@ constexpr uint32_t kOutStageBytes = kBM * 128;
 
 // A stage holds kKA "atoms" of 64 contraction elements (one 128-byte swizzle span each); the two
 // logits kernels use two atoms a stage, so that eight MMAs are queued per barrier round trip there too.
+enum UmmaMode { kModeStats = 0, kModeDz = 1, kModeDHidden = 2, kModeDW = 3,
+                kModeScores = 4, kModeScoresTop8 = 5, kModeScoresTop32 = 6, kModeDistill = 7,
+                kModeDzRow = 8, kModeDHiddenPart = 9, kModeDWBf16 = 10 };
+
+template <int kMode>
+struct ModeTraits {
+  static constexpr bool scores = (kMode >= kModeScores && kMode <= kModeScoresTop32);
+  static constexpr bool sweep = (kMode == kModeStats || scores || kMode == kModeDistill);   // units of vocabulary splits
+  static constexpr bool dz = (kMode == kModeDz || kMode == kModeDzRow);
+  static constexpr bool dh = (kMode == kModeDHidden || kMode == kModeDHiddenPart);
+  static constexpr bool dw = (kMode == kModeDW || kMode == kModeDWBf16);
+  static constexpr bool out_bf16 = dz || kMode == kModeDWBf16;        // 64-column bf16 tiles through staging
+  static constexpr bool out_f32 = (kMode == kModeDW || kMode == kModeDHiddenPart);   // 32-column float tiles
+  static constexpr int top = kMode == kModeScoresTop8 ? 8 : (kMode == kModeScoresTop32 ? 32 : 0);
+  static constexpr bool a_mn = dw;
+  static constexpr bool b_mn = dh || dw;
+  static constexpr int timing_kind = sweep ? 0 : (dz ? 1 : (dh ? 2 : 3));
+};
+
 template <int kMode, int kCta>
-struct KAtoms { static constexpr int value = (kCta == 2 && (kMode == 0 || kMode == 1)) ? 2 : 1; };
+struct KAtoms { static constexpr int value = (kCta == 2 && (ModeTraits<kMode>::sweep || ModeTraits<kMode>::dz)) ? 2 : 1; };
 
 template <int kCta, int kAcc, int kKA>
 struct PipeConfig {
@@ -61,8 +92,6 @@ struct PipeConfig {
   static constexpr size_t smem_bytes = (size_t)stages * stage_bytes + 1024 + 2 * kOutStageBytes;
 };
 constexpr long long kWaitLimitCycles = 4000000000LL;   // about two seconds at the maximum SM clock
-
-enum UmmaMode { kModeStats = 0, kModeDz = 1, kModeDHidden = 2, kModeDW = 3 };
 
 struct UmmaArgs {
   int M, N, K;              // extents of the contraction handled by this launch (valid elements)
@@ -97,12 +126,21 @@ struct UmmaArgs {
   int l2_a, l2_b;           // ptx::L2Hint of the loads of A and of B (CTA-pair kernels)
   const int* dyn_rows;      // optional device count of rows of the whole (compacted) batch: the launch then
   int dyn_base;             // covers rows [dyn_base, min(dyn_base + capacity, *dyn_rows)) of it (M, or K for d_W)
-};
-
-template <int kMode>
-struct ModeTraits {
-  static constexpr bool a_mn = (kMode == kModeDW);
-  static constexpr bool b_mn = (kMode == kModeDHidden || kMode == kModeDW);
+  // kModeScores*: partials hold (m, r, u, -), m the maximum of the raw accumulators a, r = sum 2^(c2 (a - m)) without
+  // the maximum's own 1, u = sum 2^(c2 (a - m)) c2 (a - m); targets may be NULL
+  int top_k;                // entries of a row's list that are written
+  float* top_val;           // [n_split][T_total][top_k] raw accumulators, falling; -inf where there are fewer
+  int* top_id;              // [n_split][T_total][top_k]; -1 where there are fewer
+  // kModeDistill
+  int list_k;               // slots of a row's list
+  const int* list_ids;      // [T_total][list_k] distinct ids in rising order, then INT_MAX
+  float* list_z;            // [T_total][list_k] raw accumulators at those ids
+  // kModeDzRow
+  const float4* row_p;      // (m, log2 s, alpha, beta): L = c2 (a - m) - log2 s, dz = 2^L (alpha + beta L)
+  const float* row_ins;     // dz at column targets[t]; read when targets is not NULL
+  // kModeDHiddenPart: part s covers the k-blocks [s * part_blocks, (s + 1) * part_blocks) and writes rows
+  // [s * part_rows, ...) of the output map; n_split parts
+  int part_blocks, part_rows;
 };
 
 // Raster of the (m, n) output tiles for the modes without vocabulary splits: groups of `group_m`
@@ -185,6 +223,131 @@ __device__ __forceinline__ void stats_chunk(const uint32_t (&raw)[32], int nvali
   run_u += u0 + u1;
 }
 
+// raw[idx] = -inf, likewise for an index only known at run time.
+__device__ __forceinline__ void drop_column(uint32_t (&raw)[32], int idx) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, 0fFF800000;\n\t}"
+                 : "+r"(raw[j]) : "r"(idx), "r"(j));
+}
+
+// One 32-column chunk of a row folded into (m, r, u): m the maximum so far, r the sum of 2^(c2 (a - m)) over all
+// entries but ONE that equals m, u = sum 2^(c2 (a - m)) c2 (a - m).  Leaving the maximum's own 1 out keeps the
+// relative precision of 1 - p and of the entropy in sharply peaked rows, where r is 10^-6 and would lose
+// most of its digits beside a one.  The branch on a new maximum is taken a few times per row (harmonic in the
+// number of chunks).  Entries of -inf (dropped ones) count nothing; kEnt = false leaves u alone.
+template <bool kFull, bool kEnt>
+__device__ __forceinline__ void rest_chunk(const uint32_t (&raw)[32], int nvalid, float c2, float& m, float& r, float& u) {
+  float cmax = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (kFull || j < nvalid) cmax = fmaxf(cmax, __uint_as_float(raw[j]));
+  float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
+  if (cmax > m) {
+    if (m > -INFINITY) {
+      const float d = fmaxf((m - cmax) * c2, -1000.f), sc = ex2f(d);
+      if (kEnt) u = sc * fmaf(d, r + 1.f, u);
+      r = (r + 1.f) * sc;
+    }
+    m = cmax;
+    float ties = -1.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      if (kFull || j < nvalid) {
+        const float t = (__uint_as_float(raw[j]) - m) * c2;
+        const float e = ex2f(t);
+        const bool top = __uint_as_float(raw[j]) == m;
+        ties += top ? 1.f : 0.f;
+        s0 += top ? 0.f : e;
+        if (kEnt) u0 = fmaf(e, t, u0);
+      }
+    }
+    r += s0 + ties;
+    if (kEnt) u += u0;
+    return;
+  }
+  if (!kEnt && m == -INFINITY) return;                 // nothing but dropped entries so far
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    if (kFull || j < nvalid) {
+      const float t = (__uint_as_float(raw[j]) - m) * c2;
+      const float e = ex2f(t);
+      s0 += e;
+      if (kEnt) u0 = fmaf(e, t, u0);
+    }
+    if (kFull || j + 1 < nvalid) {
+      const float t = (__uint_as_float(raw[j + 1]) - m) * c2;
+      const float e = ex2f(t);
+      s1 += e;
+      if (kEnt) u1 = fmaf(e, t, u1);
+    }
+  }
+  r += s0 + s1;
+  if (kEnt) u += u0 + u1;
+}
+
+// The kTop largest entries of a row seen so far, falling; equal values in the order they came (columns are swept in
+// rising order, so ties go to the lower id).  All indices are static, so the list stays in registers.
+template <int kTop>
+struct TopList {
+  float val[kTop];
+  int id[kTop];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < kTop; ++j) { val[j] = -INFINITY; id[j] = -1; }
+  }
+  __device__ __forceinline__ void insert(float x, int i) {
+#pragma unroll
+    for (int j = kTop - 1; j >= 0; --j) {
+      const bool here = x > val[j];                    // x belongs at j or further up
+      const bool up = j > 0 && x > val[j > 0 ? j - 1 : 0];
+      val[j] = up ? val[j > 0 ? j - 1 : 0] : (here ? x : val[j]);
+      id[j] = up ? id[j > 0 ? j - 1 : 0] : (here ? i : id[j]);
+    }
+  }
+};
+template <>
+struct TopList<0> {
+  __device__ __forceinline__ void clear() {}
+};
+
+// The entries of one chunk that beat the list's last one are taken out of the chunk one by one.  A row of N
+// entries in random order has about k (1 + ln(N / k)) of them, so most chunks only pay the comparison.
+template <int kTop>
+__device__ __forceinline__ void top_chunk(const uint32_t (&raw)[32], int nvalid, int col0, TopList<kTop>& list) {
+  uint32_t hits = 0u;
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    hits |= (__uint_as_float(raw[j]) > list.val[kTop - 1]) ? (1u << j) : 0u;
+  if (nvalid < 32) hits &= (1u << nvalid) - 1u;
+  while (hits) {
+    const int j = __ffs(hits) - 1;
+    hits &= hits - 1u;
+    const float x = pick_column(raw, j);
+    if (x > list.val[kTop - 1]) list.insert(x, col0 + j);
+  }
+}
+
+// One 32-column chunk of dz = 2^L (alpha + beta L), L = c2 (a - m) - log2 s; zero at or beyond nvalid, and for a
+// row with alpha = beta = 0 whatever its logits.
+template <bool kFull>
+__device__ __forceinline__ void dz_row_chunk(const uint32_t (&raw)[32], int nvalid, float c2, const float4& rp, bool live,
+                                             uint32_t* packed) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    float v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (kFull || j + q < nvalid) {
+        const float L = fmaf(__uint_as_float(raw[j + q]) - rp.x, c2, -rp.y);
+        v[q] = ex2f(L) * fmaf(rp.w, L, rp.z);
+      }
+    }
+    __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+    packed[j >> 1] = live ? *reinterpret_cast<uint32_t*>(&h) : 0u;
+  }
+}
+
 // One 32-column chunk of dz without its one-hot term: -coef * softmax = -sgn(coef) 2^(c2 a + k_row) with
 // k_row = log2|coef| - lse log2(e), so an element costs one fused multiply-add and one exponential; the sign
 // is applied to the packed bf16 pairs (sign_mask = 0x80008000 for coef > 0, else 0).  Columns at or beyond
@@ -216,6 +379,16 @@ __device__ __forceinline__ void put_bf16(uint32_t (&packed)[32], int idx, uint32
   }
 }
 
+// kModeDHiddenPart: unit -> output tile and the k-blocks of its part (every part has some); else all k-blocks.
+template <int kMode>
+__device__ __forceinline__ int part_of_unit(int unit, int k_blocks, const UmmaArgs& args, int& kb_begin, int& kb_end) {
+  if (kMode != kModeDHiddenPart) return unit;
+  const int tiles = args.m_tiles * args.n_tiles, part = unit / tiles;
+  kb_begin = part * args.part_blocks;
+  kb_end = min(k_blocks, kb_begin + args.part_blocks);
+  return unit - part * tiles;
+}
+
 template <int kMode, int kCta, int kAcc>
 __global__ void __launch_bounds__(kUmmaThreads, 1)
 umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -226,7 +399,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     // The number of rows is only known on the device (rows kept by the compaction of the backward):
     // this launch was sized for its capacity and shrinks itself to what is really there.
     int n = *args.dyn_rows - args.dyn_base;
-    if (kMode == kModeDW) {
+    if (ModeTraits<kMode>::dw) {
       n = n < 0 ? 0 : (n > args.K ? args.K : n);
       args.K = n;
     } else {
@@ -237,12 +410,13 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   }
   constexpr int kKA = KAtoms<kMode, kCta>::value;
   using Cfg = PipeConfig<kCta, kAcc, kKA>;
-  static_assert(kAcc == 1 || (kCta == 2 && (kMode == kModeDHidden || kMode == kModeDW)), "two accumulators: gradient modes, CTA pairs");
+  using Tr = ModeTraits<kMode>;
+  static_assert(kAcc == 1 || (kCta == 2 && (Tr::dh || Tr::dw)), "two accumulators: gradient modes, CTA pairs");
   constexpr int kBufs = 2 / kAcc;                          // tensor-memory buffers of kAcc accumulators
   constexpr int kUnitN = kBN * kAcc;                       // output columns per unit
   constexpr bool kPair = (kCta == 2);
-  constexpr bool kAmn = ModeTraits<kMode>::a_mn;
-  constexpr bool kBmn = ModeTraits<kMode>::b_mn;
+  constexpr bool kAmn = Tr::a_mn;
+  constexpr bool kBmn = Tr::b_mn;
   constexpr int kStagesT = Cfg::stages;
   constexpr int kBNcta = kBN / kCta;                       // rows of B that this CTA loads
   constexpr uint32_t kBBytesCta = kBNcta * kBK * 2;
@@ -298,7 +472,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 
   const int k_blocks = (args.K + kBK * kKA - 1) / (kBK * kKA);
   const int n_units = (k_blocks == 0) ? 0
-                      : (kMode == kModeStats) ? args.m_tiles * args.n_split : args.m_tiles * args.n_tiles;
+                      : Tr::sweep ? args.m_tiles * args.n_split
+                      : (kMode == kModeDHiddenPart) ? args.m_tiles * args.n_tiles * args.n_split
+                                                    : args.m_tiles * args.n_tiles;
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (every CTA)
@@ -314,18 +490,18 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       const uint64_t pol_a = make_l2_policy(args.l2_a);
       const uint64_t pol_b = make_l2_policy(args.l2_b);
       for (int unit = worker; unit < n_units; unit += n_workers) {
-        int m_tile, n_begin, n_end;
-        if (kMode == kModeStats) {
+        int m_tile, n_begin, n_end, kb_begin = 0, kb_end = k_blocks;
+        if (Tr::sweep) {
           m_tile = unit / args.n_split;
           stats_tile_range(args, unit % args.n_split, n_begin, n_end);
         } else {
-          unit_to_tile(unit, args, m_tile, n_begin);
+          unit_to_tile(part_of_unit<kMode>(unit, k_blocks, args, kb_begin, kb_end), args, m_tile, n_begin);
           n_end = n_begin + 1;
         }
         const int a_row = args.a_mn0 + (m_tile * kCta + cta_rank) * kBM;
         for (int n_tile = n_begin; n_tile < n_end; ++n_tile) {
           const int b_row = args.b_mn0 + n_tile * kUnitN + cta_rank * kBNcta;   // + kBN per further accumulator
-          for (int kb = 0; kb < k_blocks; ++kb) {
+          for (int kb = kb_begin; kb < kb_end; ++kb) {
             if (!mbar_wait_bounded(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_p, kWaitLimitCycles)) goto producer_drain;
             const uint32_t full = full0 + stage * (uint32_t)sizeof(uint64_t);
             if (kPair) {
@@ -418,18 +594,20 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       uint32_t acc_iter = 0;
       bool ready = false;
       for (int unit = worker; unit < n_units; unit += n_workers) {
-        int n_tiles_here = 1;
-        if (kMode == kModeStats) {
+        int n_tiles_here = 1, kb_begin = 0, kb_end = k_blocks;
+        if (Tr::sweep) {
           int n_begin, n_end;
           stats_tile_range(args, unit % args.n_split, n_begin, n_end);
           n_tiles_here = n_end - n_begin;
+        } else {
+          part_of_unit<kMode>(unit, k_blocks, args, kb_begin, kb_end);
         }
         for (int t = 0; t < n_tiles_here; ++t, ++acc_iter) {
           const uint32_t buf = acc_iter % kBufs;
           const uint32_t buf_phase = (acc_iter / kBufs) & 1u;
           if (!mbar_wait_bounded(smem_u32(&bar_tmem_empty[buf]), buf_phase ^ 1u, abort_p, kWaitLimitCycles)) goto mma_done;
           const uint32_t tmem_d = tmem_base + buf * kUnitN;
-          for (int kb = 0; kb < k_blocks; ++kb) {
+          for (int kb = kb_begin; kb < kb_end; ++kb) {
             if (!ready && !mbar_wait_bounded(smem_u32(&bar_full[stage]), phase, abort_p, kWaitLimitCycles)) goto mma_done;
             tc_fence_after_sync();
             const uint64_t da = da_base + stage * stage_step;
@@ -442,7 +620,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 for (int k = 0; k < kBK / kUmmaK; ++k) {
                   const uint64_t daq = da + t * atom_step + k * a_step;
                   const uint64_t dbq = db + t * atom_step + q * (uint64_t)(kBBytesCta >> 4) + k * b_step;
-                  const uint32_t acc = (kb > 0 || t > 0 || k > 0) ? 1u : 0u;
+                  const uint32_t acc = (kb > kb_begin || t > 0 || k > 0) ? 1u : 0u;
                   if (kPair) umma_bf16_pair(tmem_d + q * kBN, daq, dbq, idesc, acc);
                   else umma_bf16(tmem_d + q * kBN, daq, dbq, idesc, acc);
                 }
@@ -450,10 +628,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             }
             if (kPair) {
               umma_commit_pair(smem_u32(&bar_empty[stage]), 3);                        // frees the slot in both CTAs
-              if (kb == k_blocks - 1) umma_commit_pair(smem_u32(&bar_tmem_full[buf]), 3);  // accumulator ready
+              if (kb == kb_end - 1) umma_commit_pair(smem_u32(&bar_tmem_full[buf]), 3);  // accumulator ready
             } else {
               umma_commit(smem_u32(&bar_empty[stage]));
-              if (kb == k_blocks - 1) umma_commit(smem_u32(&bar_tmem_full[buf]));
+              if (kb == kb_end - 1) umma_commit(smem_u32(&bar_tmem_full[buf]));
             }
             if (++stage == kStagesT) { stage = 0; phase ^= 1u; }
             ready = mbar_try_wait(smem_u32(&bar_full[stage]), phase);
@@ -476,12 +654,14 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     uint32_t stage_iter = 0;
     for (int unit = worker; unit < n_units; unit += n_workers) {
       int m_tile, n_begin, n_end, split = 0;
-      if (kMode == kModeStats) {
+      if (Tr::sweep) {
         m_tile = unit / args.n_split;
         split = unit % args.n_split;
         stats_tile_range(args, split, n_begin, n_end);
       } else {
-        unit_to_tile(unit, args, m_tile, n_begin);
+        int kb_begin = 0, kb_end = 0;
+        unit_to_tile(part_of_unit<kMode>(unit, k_blocks, args, kb_begin, kb_end), args, m_tile, n_begin);
+        if (kMode == kModeDHiddenPart) split = unit / (args.m_tiles * args.n_tiles);
         n_end = n_begin + 1;
       }
       const int row = (m_tile * kCta + cta_rank) * kBM + row_in_tile;   // row within this launch's M extent
@@ -492,11 +672,11 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       float run_m = -INFINITY, run_s = 0.f, run_u = 0.f;
       int y = -1;
       float coef = 0.f, lse2 = 0.f;
-      if (kMode == kModeStats || kMode == kModeDz) {
+      if (kMode == kModeStats || kMode == kModeDz || ((Tr::scores || kMode == kModeDzRow) && args.targets != nullptr)) {
         if (row_ok) {
           y = args.targets[grow];
           if (y < 0 || y >= args.N) {
-            if (kMode == kModeStats) atomicOr(args.status, kStatusBadTarget);
+            if (Tr::sweep) atomicOr(args.status, kStatusBadTarget);
             y = y < 0 ? 0 : args.N - 1;
           }
         }
@@ -504,6 +684,24 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       if (kMode == kModeStats && args.resume && row_ok) {  // continue the sweep the launch before left off
         const float4 p = args.partials[(size_t)split * args.T_total + grow];
         run_m = p.x; run_s = p.y; run_u = p.z;
+      }
+      [[maybe_unused]] TopList<Tr::top> list;
+      if constexpr (Tr::top > 0) list.clear();
+      [[maybe_unused]] int list_pos = 0, next_id = INT_MAX;   // kModeDistill: the next id of the row's list in this sweep
+      if (kMode == kModeDistill && row_ok) {
+        const int* ids = args.list_ids + (size_t)grow * args.list_k;
+        int hi = args.list_k;
+        while (list_pos < hi) {                               // first id at or behind the split's first column
+          const int mid = (list_pos + hi) >> 1;
+          if (ids[mid] < n_begin * kUnitN) list_pos = mid + 1; else hi = mid;
+        }
+        if (list_pos < args.list_k) next_id = ids[list_pos];
+      }
+      [[maybe_unused]] float4 rp = make_float4(0.f, 0.f, 0.f, 0.f);   // kModeDzRow
+      [[maybe_unused]] float ins = 0.f;
+      if (kMode == kModeDzRow && row_ok) {
+        rp = args.row_p[grow];
+        if (args.targets != nullptr) ins = args.row_ins[grow];
       }
       float k_row = -INFINITY;                          // kModeDz: log2|coef| - lse log2(e); -inf gives a zero row
       uint32_t sign_mask = 0u;
@@ -528,7 +726,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           goto role_done;
         tc_fence_after_sync();
         const uint32_t taddr = tmem_base + buf * kUnitN + ((uint32_t)(quarter * 32) << 16);
-        if (kMode == kModeDz) {
+        if (Tr::out_bf16) {
           // 64 columns (one 128-byte row of bf16) at a time: two accumulator chunks -> packed registers ->
           // swizzled staging tile in shared memory -> one TMA store of 128 rows x 128 bytes, so that the
           // panel is written in whole lines by the copy engine instead of 16 bytes a thread
@@ -544,11 +742,31 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             tmem_ld_wait();
             uint32_t packed[32];
             const int nv0 = args.N - col0, nv1 = args.N - col0 - 32;
-            if (nv0 >= 32) dz_chunk<true>(raw0, 32, c2, k_row, sign_mask, packed);
-            else dz_chunk<false>(raw0, nv0, c2, k_row, sign_mask, packed);
-            if (nv1 >= 32) dz_chunk<true>(raw1, 32, c2, k_row, sign_mask, packed + 16);
-            else dz_chunk<false>(raw1, nv1, c2, k_row, sign_mask, packed + 16);
-            if (row_ok && y >= col0 && y < col0 + 64) {        // the one-hot term: coef (1 - p_y) at the target column
+            if (kMode == kModeDz) {
+              if (nv0 >= 32) dz_chunk<true>(raw0, 32, c2, k_row, sign_mask, packed);
+              else dz_chunk<false>(raw0, nv0, c2, k_row, sign_mask, packed);
+              if (nv1 >= 32) dz_chunk<true>(raw1, 32, c2, k_row, sign_mask, packed + 16);
+              else dz_chunk<false>(raw1, nv1, c2, k_row, sign_mask, packed + 16);
+            } else if (kMode == kModeDzRow) {
+              const bool live = rp.z != 0.f || rp.w != 0.f;
+              if (nv0 >= 32) dz_row_chunk<true>(raw0, 32, c2, rp, live, packed);
+              else dz_row_chunk<false>(raw0, nv0, c2, rp, live, packed);
+              if (nv1 >= 32) dz_row_chunk<true>(raw1, 32, c2, rp, live, packed + 16);
+              else dz_row_chunk<false>(raw1, nv1, c2, rp, live, packed + 16);
+              if (row_ok && y >= col0 && y < col0 + 64) {
+                const __nv_bfloat16 hv = __float2bfloat16_rn(ins);
+                put_bf16(packed, y - col0, (uint32_t)(*reinterpret_cast<const uint16_t*>(&hv)));
+              }
+            } else {                                           // kModeDWBf16
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                __nv_bfloat162 h0 = __floats2bfloat162_rn(__uint_as_float(raw0[j]), __uint_as_float(raw0[j + 1]));
+                __nv_bfloat162 h1 = __floats2bfloat162_rn(__uint_as_float(raw1[j]), __uint_as_float(raw1[j + 1]));
+                packed[j >> 1] = *reinterpret_cast<uint32_t*>(&h0);
+                packed[16 + (j >> 1)] = *reinterpret_cast<uint32_t*>(&h1);
+              }
+            }
+            if (kMode == kModeDz && row_ok && y >= col0 && y < col0 + 64) {        // the one-hot term: coef (1 - p_y) at the target column
               const int idx = y - col0;
               const float ay = idx < 32 ? pick_column(raw0, idx) : pick_column(raw1, idx - 32);
               const float vy = coef * (1.f - ex2f(fmaf(ay, c2, -lse2)));
@@ -569,13 +787,14 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             fence_async_proxy();
             epilogue_bar_sync();
             if (issuer) {
-              tma_store_2d(&map_c, out_buf, col0, tile_row);   // rows past the panel's capacity are clipped
+              // rows past the panel's capacity (d_W: past the vocabulary) are clipped
+              if (Tr::dz || tile_row < args.M) tma_store_2d(&map_c, out_buf, col0, (Tr::dz ? 0 : args.row0) + tile_row);
               bulk_commit_group();
             }
           }
         }
 #pragma unroll 1
-        for (int c = 0; kMode != kModeDz && c < kUnitN / 32; ++c) {
+        for (int c = 0; !Tr::out_bf16 && c < kUnitN / 32; ++c) {
           const int col0 = col_base + c * 32;
           if (col0 >= args.N) break;                           // whole chunk beyond the valid columns
           const int nvalid = min(32, args.N - col0);
@@ -589,6 +808,24 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             if (row_ok && y >= col0 && y < col0 + 32) {
               args.acc_y[grow] = pick_column(raw, y - col0);
             }
+          } else if constexpr (Tr::scores) {
+            if (nvalid >= 32) rest_chunk<true, true>(raw, 32, c2, run_m, run_s, run_u);
+            else rest_chunk<false, true>(raw, nvalid, c2, run_m, run_s, run_u);
+            if constexpr (Tr::top > 0) {
+              if (row_ok) top_chunk<Tr::top>(raw, nvalid, col0, list);
+              __syncwarp();                                      // the next tensor-memory load is the whole warp's
+            }
+            if (row_ok && y >= col0 && y < col0 + 32) args.acc_y[grow] = pick_column(raw, y - col0);
+          } else if constexpr (kMode == kModeDistill) {
+            while (next_id < col0 + 32) {                        // INT_MAX: no more ids, or no row
+              args.list_z[(size_t)grow * args.list_k + list_pos] = pick_column(raw, next_id - col0);
+              drop_column(raw, next_id - col0);
+              ++list_pos;
+              next_id = list_pos < args.list_k ? args.list_ids[(size_t)grow * args.list_k + list_pos] : INT_MAX;
+            }
+            __syncwarp();                                        // the next tensor-memory load is the whole warp's
+            if (nvalid >= 32) rest_chunk<true, false>(raw, 32, c2, run_m, run_s, run_u);
+            else rest_chunk<false, false>(raw, nvalid, c2, run_m, run_s, run_u);
           } else if (kMode == kModeDHidden) {
             if (row_ok) {
               uint32_t packed[16];
@@ -602,7 +839,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
               for (int q = 0; q < 4; ++q)
                 if (q * 8 < nvalid) dst[q] = make_uint4(packed[4 * q], packed[4 * q + 1], packed[4 * q + 2], packed[4 * q + 3]);
             }
-          } else {  // kModeDW: swizzled staging tile, then one TMA store (first panel) or reduce-add
+          } else {  // kModeDW, kModeDHiddenPart: swizzled staging tile, then one TMA store (first panel) or reduce-add
             const uint32_t out_buf = smem_base + kStagesT * kStageBytesCta + (stage_iter++ & 1u) * kOutStageBytes;
             const bool issuer = (threadIdx.x == 64);             // first thread of the epilogue warps
             if (issuer) bulk_wait_read_le1();                    // the copy that last read this tile is done with it
@@ -619,7 +856,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             epilogue_bar_sync();
             if (issuer) {
               const int tile_row = (m_tile * kCta + cta_rank) * kBM;      // rows past M never reach memory
-              if (tile_row < args.M) {
+              if (kMode == kModeDHiddenPart) {                             // rows past M: padding of the part
+                tma_store_2d(&map_c, out_buf, col0, split * args.part_rows + tile_row);
+              } else if (tile_row < args.M) {
                 if (args.accumulate) tma_reduce_add_2d(&map_c, out_buf, col0, args.row0 + tile_row);
                 else tma_store_2d(&map_c, out_buf, col0, args.row0 + tile_row);
               }
@@ -636,13 +875,22 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         }
       }
 
-      if (kMode == kModeStats && row_ok)
+      if constexpr (Tr::top > 0) {
+        if (row_ok) {
+          float* tv = args.top_val + ((size_t)split * args.T_total + grow) * args.top_k;
+          int* ti = args.top_id + ((size_t)split * args.T_total + grow) * args.top_k;
+#pragma unroll
+          for (int j = 0; j < Tr::top; ++j)
+            if (j < args.top_k) { tv[j] = list.val[j]; ti[j] = list.id[j]; }
+        }
+      }
+      if (Tr::sweep && row_ok)
         args.partials[(size_t)split * args.T_total + grow] = make_float4(run_m, run_s, run_u, 0.f);
     }
   }
 
 role_done:
-  if ((kMode == kModeDW || kMode == kModeDz) && threadIdx.x == 64) bulk_wait_all();   // the tile copies have left shared memory and landed
+  if ((Tr::out_bf16 || Tr::out_f32) && threadIdx.x == 64) bulk_wait_all();   // the tile copies have left shared memory and landed
   if (*abort_p && lane == 0) atomicOr(args.status, kStatusTimeout);
   tc_fence_before_sync();
   __syncthreads();

@@ -1,0 +1,266 @@
+"""Token scores and distillation on the LM head: argument checks and marshalling for libulorl.so.
+
+token_scores       log-prob of given tokens, entropy and the most likely alternatives from hidden states and W
+                   (what a rollout records as old_logp, a reference policy as ref_logp, a teacher for its student)
+token_scores_bwd   gradients of a caller's loss on those log-probs and entropies
+logits_scores      the same scores from logits that are already there (a decoding step)
+distill_fwd/_bwd   distillation from a teacher's top logits
+
+Calls run on the current stream of the tensors' device and never synchronise; findings of the kernels are read with
+binding.check_status(workspace).  There is no CPU path.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from dataclasses import dataclass
+from typing import Optional
+
+import torch
+
+from .binding import BF16, F32, OK, CHeadParams, UlorlError, _PATH, load_library, status_string
+
+MAX_TOP, MAX_LIST = 32, 128
+_DISTILL = {"raw": 0, "renorm": 1, "tail": 2}
+_DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+_LOGITS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: 2}
+
+
+@dataclass
+class HeadParams:
+    """Mirror of ulorl_head_params_t.  top_k: alternatives that token_scores returns, or entries of a teacher's list."""
+    T: int
+    H: int
+    V: int
+    dtype: str = "bf16"
+    top_k: int = 0
+    kernel_path: str = "auto"
+    inv_temperature: float = 1.0
+    bwd_panel_tokens: int = 0
+    dw_accumulate: bool = False
+    dw_dtype: str = "f32"
+    distill_mode: str = "raw"
+    teacher_inv_temperature: float = 1.0
+    norm_tokens: int = 0
+
+    def to_c(self) -> CHeadParams:
+        for name, value, known in (("dtype", self.dtype, _DTYPES), ("dw_dtype", self.dw_dtype, _DTYPES),
+                                   ("kernel_path", self.kernel_path, _PATH), ("distill_mode", self.distill_mode, _DISTILL)):
+            if value not in known:
+                raise UlorlError(f"{name}: {value!r} is not one of {sorted(known)}")
+        return CHeadParams(self.T, self.H, self.V, BF16 if self.dtype == "bf16" else F32, self.top_k,
+                           _PATH[self.kernel_path], self.inv_temperature, self.bwd_panel_tokens, int(self.dw_accumulate),
+                           BF16 if self.dw_dtype == "bf16" else F32, _DISTILL[self.distill_mode],
+                           self.teacher_inv_temperature, self.norm_tokens)
+
+
+@dataclass
+class ScoresOut:
+    logp: Optional[torch.Tensor]         # [T], None without targets
+    entropy: torch.Tensor                # [T]
+    lse: torch.Tensor                    # [T]
+    norm: Optional[torch.Tensor]         # [T, 2], read by token_scores_bwd; None from logits_scores
+    top_ids: Optional[torch.Tensor]      # [T, top_k] int32, None with top_k = 0
+    top_logp: Optional[torch.Tensor]     # [T, top_k]
+
+
+@dataclass
+class DistillOut:
+    loss: torch.Tensor                   # [1]
+    kl: torch.Tensor                     # [T]
+    lse: torch.Tensor                    # [T]
+    norm: torch.Tensor                   # [T, 2], and with it for distill_bwd:
+    coef: torch.Tensor                   # [T]
+    entry_grad: torch.Tensor             # [T, top_k]
+
+
+def _raise(code: int, what: str):
+    raise UlorlError(f"{what} failed: {status_string(code)} ({code})")
+
+
+def _take(t: Optional[torch.Tensor], name: str, dtype, n: int, device, optional: bool = False):
+    """The tensor's device pointer, after the checks that keep the kernels inside it."""
+    if t is None:
+        if optional:
+            return None
+        raise UlorlError(f"{name} is missing")
+    if t.dtype != dtype or t.numel() != n:
+        raise UlorlError(f"{name}: expected {n} elements of {dtype}, got {t.numel()} of {t.dtype}")
+    if t.device != device or not t.is_contiguous():
+        raise UlorlError(f"{name}: expected a contiguous tensor on {device}")
+    return t.data_ptr()
+
+
+def _device_of(t: torch.Tensor, name: str):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise UlorlError(f"{name}: expected a CUDA tensor (there is no CPU path)")
+    return t.device
+
+
+def _on(device):
+    """Makes the tensors' device the current one for the call, if it is not."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _stream(device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def head_workspace_bytes(p: HeadParams, backward: bool = True) -> int:
+    n = load_library().ulorl_head_workspace_bytes(ctypes.byref(p.to_c()), int(backward))
+    if n == 0:
+        raise UlorlError("ulorl_head_workspace_bytes: invalid parameters")
+    return int(n)
+
+
+def alloc_head_workspace(p: HeadParams, device, backward: bool = True) -> torch.Tensor:
+    """Scratch of the calls with these params; backward=False is enough (and far smaller) for the forward ones."""
+    with _on(torch.device(device)) if torch.device(device).index is not None else contextlib.nullcontext():
+        return torch.empty(head_workspace_bytes(p, backward), dtype=torch.uint8, device=device)
+
+
+def _workspace(p: HeadParams, workspace, device, backward: bool):
+    if workspace is None:
+        workspace = alloc_head_workspace(p, device, backward)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise UlorlError(f"workspace: expected a contiguous tensor on {device}")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _operands(p: HeadParams, hidden, W):
+    device = _device_of(hidden, "hidden")
+    dtype = _DTYPES.get(p.dtype)
+    return device, _take(hidden, "hidden", dtype, p.T * p.H, device), _take(W, "W", dtype, p.V * p.H, device)
+
+
+def token_scores(p: HeadParams, hidden, W, targets=None, out: Optional[ScoresOut] = None,
+                 workspace: Optional[torch.Tensor] = None) -> ScoresOut:
+    """ulorl_token_scores on the current stream of the tensors' device."""
+    lib = load_library()
+    cp = p.to_c()
+    device, ph, pw = _operands(p, hidden, W)
+    pt = _take(targets, "targets", torch.int32, p.T, device, optional=True)
+    f32, T, k = torch.float32, p.T, p.top_k
+    with _on(device):
+        if out is None:
+            rows = torch.empty(5, T, dtype=f32, device=device)
+            # norm first: pairs need eight-byte alignment
+            out = ScoresOut(rows[2] if targets is not None else None, rows[3], rows[4], rows[:2].view(T, 2),
+                            torch.empty(T, k, dtype=torch.int32, device=device) if k else None,
+                            torch.empty(T, k, dtype=f32, device=device) if k else None)
+        workspace, pws, nws = _workspace(p, workspace, device, False)
+        code = lib.ulorl_token_scores(
+            ctypes.byref(cp), ph, pw, pt, _take(out.logp, "logp", f32, T, device, targets is None),
+            _take(out.entropy, "entropy", f32, T, device, True), _take(out.lse, "lse", f32, T, device, True),
+            _take(out.norm, "norm", f32, 2 * T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k == 0),
+            _take(out.top_logp, "top_logp", f32, T * k, device, k == 0), pws, nws, _stream(device))
+    if code != OK:
+        _raise(code, "ulorl_token_scores")
+    return out
+
+
+def _grad_outputs(p: HeadParams, d_hidden, d_W, hidden, device):
+    if d_hidden is None:
+        d_hidden = torch.empty_like(hidden)
+    if d_W is None:
+        d_W = (torch.zeros if p.dw_accumulate else torch.empty)(p.V, p.H, dtype=_DTYPES[p.dw_dtype], device=device)
+    return (d_hidden, d_W, _take(d_hidden, "d_hidden", _DTYPES[p.dtype], p.T * p.H, device),
+            _take(d_W, "d_W", _DTYPES[p.dw_dtype], p.V * p.H, device))
+
+
+def token_scores_bwd(p: HeadParams, hidden, W, targets, scores: ScoresOut, d_logp=None, d_entropy=None, d_hidden=None,
+                     d_W=None, workspace: Optional[torch.Tensor] = None):
+    """ulorl_token_scores_bwd: (d_hidden, d_W) for d loss / d logp and d loss / d entropy (None = zero), given what
+    token_scores returned for the same operands."""
+    lib = load_library()
+    cp = p.to_c()
+    device, ph, pw = _operands(p, hidden, W)
+    f32, T = torch.float32, p.T
+    with _on(device):
+        d_hidden, d_W, pdh, pdw = _grad_outputs(p, d_hidden, d_W, hidden, device)
+        workspace, pws, nws = _workspace(p, workspace, device, True)
+        code = lib.ulorl_token_scores_bwd(
+            ctypes.byref(cp), ph, pw, _take(targets, "targets", torch.int32, T, device, d_logp is None),
+            _take(scores.norm, "norm", f32, 2 * T, device), _take(scores.logp, "logp", f32, T, device, d_logp is None),
+            _take(scores.entropy, "entropy", f32, T, device, d_entropy is None),
+            _take(d_logp, "d_logp", f32, T, device, True), _take(d_entropy, "d_entropy", f32, T, device, True),
+            pdh, pdw, pws, nws, _stream(device))
+    if code != OK:
+        _raise(code, "ulorl_token_scores_bwd")
+    return d_hidden, d_W
+
+
+def logits_scores(logits: torch.Tensor, targets=None, top_k: int = 0, inv_temperature: float = 1.0,
+                  out: Optional[ScoresOut] = None) -> ScoresOut:
+    """ulorl_logits_scores: scores from logits [T, V] (float32, bfloat16 or float16; rows may be strided)."""
+    lib = load_library()
+    device = _device_of(logits, "logits")
+    code = _LOGITS.get(logits.dtype)
+    if code is None or logits.dim() != 2 or logits.shape[1] == 0:
+        raise UlorlError("logits: expected float32, bfloat16 or float16 [T, V]")
+    T, V = logits.shape
+    ld = logits.stride(0) if T > 1 else V
+    if (V > 1 and logits.stride(1) != 1) or ld < V:
+        raise UlorlError("logits: a row must be contiguous and rows must not overlap")
+    pt = _take(targets, "targets", torch.int32, T, device, optional=True)
+    f32, k = torch.float32, top_k
+    with _on(device):
+        if out is None:
+            rows = torch.empty(3, T, dtype=f32, device=device)
+            out = ScoresOut(rows[0] if targets is not None else None, rows[1], rows[2], None,
+                            torch.empty(T, k, dtype=torch.int32, device=device) if k > 0 else None,
+                            torch.empty(T, k, dtype=f32, device=device) if k > 0 else None)
+        code = lib.ulorl_logits_scores(
+            logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
+            _take(out.logp, "logp", f32, T, device, targets is None), _take(out.entropy, "entropy", f32, T, device, True),
+            _take(out.lse, "lse", f32, T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k <= 0),
+            _take(out.top_logp, "top_logp", f32, T * k, device, k <= 0), _stream(device))
+    if code != OK:
+        _raise(code, "ulorl_logits_scores")
+    return out
+
+
+def distill_fwd(p: HeadParams, hidden, W, teacher_ids, teacher_logp, weights=None, out: Optional[DistillOut] = None,
+                workspace: Optional[torch.Tensor] = None) -> DistillOut:
+    """ulorl_distill_fwd: loss of the student's softmax against the teacher's top_k entries per token."""
+    lib = load_library()
+    cp = p.to_c()
+    device, ph, pw = _operands(p, hidden, W)
+    f32, T, k = torch.float32, p.T, p.top_k
+    pi = _take(teacher_ids, "teacher_ids", torch.int32, T * k, device)
+    pl = _take(teacher_logp, "teacher_logp", f32, T * k, device)
+    pwt = _take(weights, "weights", f32, T, device, optional=True)
+    with _on(device):
+        if out is None:
+            rows = torch.empty(5, T, dtype=f32, device=device)
+            out = DistillOut(torch.empty(1, dtype=f32, device=device), rows[2], rows[3], rows[:2].view(T, 2), rows[4],
+                             torch.empty(T, k, dtype=f32, device=device))
+        workspace, pws, nws = _workspace(p, workspace, device, False)
+        code = lib.ulorl_distill_fwd(
+            ctypes.byref(cp), ph, pw, pi, pl, pwt, _take(out.loss, "loss", f32, 1, device), _take(out.kl, "kl", f32, T, device),
+            _take(out.lse, "lse", f32, T, device, True), _take(out.norm, "norm", f32, 2 * T, device),
+            _take(out.coef, "coef", f32, T, device), _take(out.entry_grad, "entry_grad", f32, T * k, device), pws, nws,
+            _stream(device))
+    if code != OK:
+        _raise(code, "ulorl_distill_fwd")
+    return out
+
+
+def distill_bwd(p: HeadParams, hidden, W, teacher_ids, fwd: DistillOut, grad_loss=None, d_hidden=None, d_W=None,
+                workspace: Optional[torch.Tensor] = None):
+    """ulorl_distill_bwd: (d_hidden, d_W) given what distill_fwd returned for the same operands."""
+    lib = load_library()
+    cp = p.to_c()
+    device, ph, pw = _operands(p, hidden, W)
+    f32, T, k = torch.float32, p.T, p.top_k
+    with _on(device):
+        d_hidden, d_W, pdh, pdw = _grad_outputs(p, d_hidden, d_W, hidden, device)
+        workspace, pws, nws = _workspace(p, workspace, device, True)
+        code = lib.ulorl_distill_bwd(
+            ctypes.byref(cp), ph, pw, _take(teacher_ids, "teacher_ids", torch.int32, T * k, device),
+            _take(fwd.norm, "norm", f32, 2 * T, device), _take(fwd.coef, "coef", f32, T, device),
+            _take(fwd.entry_grad, "entry_grad", f32, T * k, device), _take(grad_loss, "grad_loss", f32, 1, device, True),
+            pdh, pdw, pws, nws, _stream(device))
+    if code != OK:
+        _raise(code, "ulorl_distill_bwd")
+    return d_hidden, d_W
