@@ -360,7 +360,7 @@ typedef struct {
   int32_t top_k;               /* scores: alternatives returned per token (0 .. ULORL_MAX_TOP, at most V);         */
                                /* distillation: entries per token of the teacher's list (1 .. ULORL_MAX_LIST)      */
   int32_t kernel_path;         /* AUTO, SIMT or TENSOR                                                             */
-  float inv_temperature;       /* kappa multiplying the logits                                                     */
+  float inv_temperature;       /* kappa multiplying the logits; at most 1e6                                        */
   int32_t bwd_panel_tokens;    /* backward: tokens per staging panel; 0 = library default                          */
   int32_t dw_accumulate;       /* backward: 0 overwrite d_W, 1 add into it                                         */
   int32_t dw_dtype;            /* ulorl_dtype_t of d_W                                                             */

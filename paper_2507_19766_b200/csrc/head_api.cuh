@@ -5,19 +5,20 @@
 
 namespace ulorl {
 
-constexpr int kHeadMaxSplits = 128;        // merge_scores_kernel walks up to four lists a lane
+constexpr int kHeadMaxSplits = kMaxRowLists / 2;   // a split leaves two partial results of a row
 
 struct HeadPlan {
   bool tensor;
   int sms, workers;                        // workers: CTA pairs
   int n_split, tiles_per_split;            // vocabulary splits of the forward sweep
+  int n_partial;                           // partial results of a row that it leaves
   int panel_tokens, n_panels;
   size_t dz_ld;
   bool dw_direct;                          // d_W leaves the contraction as bf16: one panel, nothing to add to
   bool dw_acc;                             // d_W summed in float32 in the workspace, rounded at the end
   int dh_parts, dh_part_blocks, dh_part_rows;
   // forward scratch
-  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_sorted, off_slots, off_list_z, fwd_total;
+  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_top_pub, off_sorted, off_slots, off_list_z, fwd_total;
   // backward scratch, over the same bytes
   size_t off_row_p, off_row_ins, off_panel, off_dw_acc, off_parts, bwd_total;
 };
@@ -33,6 +34,7 @@ static int validate_head(const ulorl_head_params_t* p) {
   if (p->kernel_path == ULORL_PATH_TENSOR_1CTA) return ULORL_ERR_UNSUPPORTED;
   if (p->kernel_path == ULORL_PATH_TENSOR && p->dtype != ULORL_BF16) return ULORL_ERR_UNSUPPORTED;
   if (!(p->inv_temperature > 0.f) || !std::isfinite(p->inv_temperature)) return ULORL_ERR_INVALID_ARG;
+  if (p->inv_temperature > 1e6f) return ULORL_ERR_UNSUPPORTED;      // exponents of absent columns have to stay finite
   if (!(p->teacher_inv_temperature > 0.f) || !std::isfinite(p->teacher_inv_temperature)) return ULORL_ERR_INVALID_ARG;
   if (p->distill_mode < ULORL_DISTILL_RAW || p->distill_mode > ULORL_DISTILL_TAIL) return ULORL_ERR_INVALID_ARG;
   if (p->distill_mode != ULORL_DISTILL_RENORM && p->teacher_inv_temperature != 1.f) return ULORL_ERR_INVALID_ARG;
@@ -56,28 +58,33 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   pl.n_split = 1;
   pl.tiles_per_split = n_tiles;
   if (pl.tensor) {
-    // As for the policy loss: as few splits as keep the live hidden tiles in L2, then the best wave quantisation
-    // among the next few.  Unlike there the splits of a small batch go up to the worker count, so that every
-    // SM streams its share of W.
-    int want = (8 * pl.workers + m_tiles - 1) / m_tiles;
-    want = std::min(want, pl.workers);
+    // As for the policy loss: enough splits that the live hidden tiles stay in L2, then the count with the shortest
+    // modelled time, waves of units x time of a unit, the fewest splits within one percent.  A unit's time is that
+    // of its contractions (8 H cycles a tile) or that of its epilogue, whichever is longer: about 2400 cycles a tile
+    // and, with alternatives, the entries that enter a row's list, k (1 + ln(columns / k)) of them, some 2.5 times as
+    // many insertions for the warp's 32 rows together.  A list starts anew in every split, so short splits pay most:
+    // 1537 tokens x 32768 entries, H 1024, k 8: 251 us with 64 splits of two tiles.
+    const double insertion = 1.5 * (p->top_k <= 8 ? 80.0 : 250.0);
+    const int list = p->top_k <= 0 ? 0 : (p->top_k <= 8 ? 8 : kMaxTop);
     const size_t live_bytes = (size_t)pl.workers * (size_t)tile_m * (size_t)H * 2;
-    const int fit = (int)((live_bytes + kStatsHiddenBudget - 1) / kStatsHiddenBudget);
-    want = std::max(1, std::min(std::max(want, fit), std::min(kHeadMaxSplits, n_tiles)));
+    const int s_max = std::min(kHeadMaxSplits, n_tiles);
+    const int s_min = std::max(1, std::min((int)((live_bytes + kStatsHiddenBudget - 1) / kStatsHiddenBudget), s_max));
     auto cost_of = [&](int s) {
       const int tps = (n_tiles + s - 1) / s;
       const int s_eff = (n_tiles + tps - 1) / tps;
-      const long waves = ((long)m_tiles * s_eff + pl.workers - 1) / pl.workers;
-      return waves * tps;
+      const double columns = std::min((double)tps * kBN, (double)V);
+      const double enters = list ? list * (1.0 + std::log(std::max(1.0, columns / list))) : 0.0;
+      const double unit = std::max(tps * 8.0 * H, tps * 4000.0 + enters * insertion);
+      return (double)(((long)m_tiles * s_eff + pl.workers - 1) / pl.workers) * unit;
     };
-    const int s_max = std::min(std::min(want + 3, kHeadMaxSplits), n_tiles);
-    long best = cost_of(want);
-    for (int s = want + 1; s <= s_max; ++s) best = std::min(best, cost_of(s));
-    for (int s = want; s <= s_max; ++s)
-      if (cost_of(s) * 100 <= best * 101) { want = s; break; }
+    double best = cost_of(s_min);
+    for (int s = s_min + 1; s <= s_max; ++s) best = std::min(best, cost_of(s));
+    int want = s_min;
+    while (want < s_max && cost_of(want) > best * 1.01) ++want;
     pl.tiles_per_split = (n_tiles + want - 1) / want;
     pl.n_split = (n_tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
   }
+  pl.n_partial = pl.tensor ? 2 * pl.n_split : 1;
   // backward panels
   int panel = p->bwd_panel_tokens > 0 ? p->bwd_panel_tokens : (pl.tensor ? pl.workers * tile_m : kDefaultPanelSimt);
   if (!pl.tensor) panel = std::min(panel, 32768);                   // rows are a grid dimension there
@@ -103,10 +110,11 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   }
   size_t off = 256;
   pl.off_status = 0;
-  pl.off_partials = off;  off = align_up(off + sizeof(float4) * (size_t)pl.n_split * T1, 256);
+  pl.off_partials = off;  off = align_up(off + sizeof(float4) * (size_t)pl.n_partial * T1, 256);
   pl.off_acc_y = off;     off = align_up(off + sizeof(float) * T1, 256);
-  pl.off_top_val = off;   off = align_up(off + sizeof(float) * (size_t)pl.n_split * T1 * K, 256);
-  pl.off_top_id = off;    off = align_up(off + sizeof(int) * (size_t)pl.n_split * T1 * K, 256);
+  pl.off_top_val = off;   off = align_up(off + sizeof(float) * (size_t)pl.n_partial * T1 * K, 256);
+  pl.off_top_id = off;    off = align_up(off + sizeof(int) * (size_t)pl.n_partial * T1 * K, 256);
+  pl.off_top_pub = off;   off = align_up(off + (K ? sizeof(uint32_t) * (size_t)std::min(pl.n_partial, 32) * T1 : 0), 256);
   pl.off_sorted = off;    off = align_up(off + sizeof(int) * T1 * K, 256);
   pl.off_list_z = off;    off = align_up(off + sizeof(float) * T1 * K, 256);
   pl.off_slots = off;     off = align_up(off + T1 * K, 1024);
@@ -369,10 +377,13 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
     a.top_k = k;
     a.top_val = reinterpret_cast<float*>(ws + pl.off_top_val);
     a.top_id = reinterpret_cast<int*>(ws + pl.off_top_id);
+    a.top_pub = reinterpret_cast<uint32_t*>(ws + pl.off_top_pub);
+    if (k > 0 && cudaMemsetAsync(a.top_pub, 0, sizeof(uint32_t) * (size_t)std::min(pl.n_partial, 32) * (size_t)T, stream) != cudaSuccess)
+      return ULORL_ERR_CUDA;
     st = run_sweep(params, pl, k == 0 ? kModeScores : (k <= 8 ? kModeScoresTop8 : kModeScoresTop32), a, hidden, W, ws, stream);
     if (st != ULORL_OK) return st;
     MergeArgs m{};
-    m.T = T; m.n_split = pl.n_split; m.k = k;
+    m.T = T; m.n_split = pl.n_partial; m.k = k;
     m.kappa = params->inv_temperature;
     m.partials = reinterpret_cast<const float4*>(ws + pl.off_partials);
     m.acc_y = a.acc_y;
@@ -380,10 +391,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
     m.logp = logp; m.entropy = entropy; m.lse = lse;
     m.norm = reinterpret_cast<float2*>(norm);
     m.out_ids = top_ids; m.out_logp = top_logp;
-    const size_t per_warp = sizeof(unsigned long long) * (size_t)pl.n_split * (size_t)k;   // at most 32 KB
-    int warps = 8;
-    while (warps > 1 && per_warp * warps > 48u * 1024u) warps /= 2;
-    merge_scores_kernel<<<(T + warps - 1) / warps, warps * 32, per_warp * warps, stream>>>(m);
+    merge_scores_kernel<<<(T + kMergeWarps - 1) / kMergeWarps, 32 * kMergeWarps, 0, stream>>>(m);
     return check_launch();
   }
   float* panel = reinterpret_cast<float*>(ws + pl.off_panel);
@@ -510,7 +518,7 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
     }
   }
   DistillRowArgs d{};
-  d.T = T; d.K = K; d.n_split = pl.n_split; d.mode = params->distill_mode;
+  d.T = T; d.K = K; d.n_split = pl.n_partial; d.mode = params->distill_mode;
   d.kappa = params->inv_temperature;
   d.teacher_kappa = params->teacher_inv_temperature;
   d.inv_N = 1.0 / (params->norm_tokens > 0 ? (double)params->norm_tokens : (double)T);

@@ -19,6 +19,7 @@ namespace ulorl {
 
 constexpr int kMaxTop = 32;            // alternatives a scoring call returns
 constexpr int kMaxList = 128;          // entries of a teacher's list
+constexpr int kMaxRowLists = 160;      // partial results of a row that the merge takes
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -426,10 +427,13 @@ __device__ __forceinline__ void merge_partials(const float4* __restrict__ partia
   if (at_max > 1) r += (float)(at_max - 1);
 }
 
-__global__ void merge_scores_kernel(const MergeArgs a) {
-  extern __shared__ unsigned long long sh_lists[];                  // per warp [n_split * k]
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int t = blockIdx.x * warps + warp;
+constexpr int kMergeCandidates = 256;
+constexpr int kMergeWarps = 8;
+
+__global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const MergeArgs a) {
+  __shared__ unsigned long long sh_lists[kMergeWarps * kMergeCandidates];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * kMergeWarps + warp;
   if (t >= a.T) return;
   float M, r, u;
   merge_partials(a.partials, a.n_split, a.T, t, a.kappa * kLog2e, M, r, u);
@@ -441,44 +445,98 @@ __global__ void merge_scores_kernel(const MergeArgs a) {
     if (a.logp) a.logp[t] = a.kappa * (a.acc_y[t] - M) - ln_s;
   }
   if (a.k == 0) return;
-  // every split's list falls: lane l walks the lists of splits l, l + 32, ..., the warp takes the best head k times
-  unsigned long long* mine = sh_lists + (size_t)warp * a.n_split * a.k;
-  for (int i = lane; i < a.n_split * a.k; i += 32) {
-    const size_t at = ((size_t)(i / a.k) * a.T + t) * a.k + i % a.k;
-    const int id = a.top_id[at];
-    mine[i] = id < 0 ? 0ull : pack_entry(order_key(a.top_val[at]), id);
+  // The lists fall.  The k-th largest of the first q entries of every list, at least 2 k of them, bounds the row's top
+  // from below: what is below it stays out, the rest (a few more than k) is ranked by counting.
+  unsigned long long* cand = sh_lists + (size_t)warp * kMergeCandidates;
+  const size_t stride = (size_t)a.T * a.k;
+  const float* val = a.top_val + (size_t)t * a.k;
+  const int* id = a.top_id + (size_t)t * a.k;
+  constexpr int kHeads = (2 * kMaxTop + kMaxRowLists + 31) / 32;
+  const int q = min(a.k, (2 * a.k + a.n_split - 1) / a.n_split), heads = q * a.n_split;
+  uint32_t key[kHeads];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int j = i * 32 + lane;
+    key[i] = j < heads ? order_key(val[(j / q) * stride + j % q]) : 0u;
+  }
+  uint32_t least = 0u;
+#pragma unroll 1
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t c = least | (1u << bit);
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i)
+      if (i * 32 < heads) count += __popc(__ballot_sync(0xffffffffu, key[i] >= c));
+    if (count >= a.k) least = c;
+  }
+  const int width = a.k <= 8 ? 8 : (a.k <= 16 ? 16 : 32), per = 32 / width;      // lists a round takes
+  const int e = lane % width, l0 = lane / width;
+  int n = 0;
+  constexpr int kAhead = 6;                                         // loads in flight: the rounds depend on each other only by n
+  for (int l = 0; l < a.n_split; l += per * kAhead) {
+    float x[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int at = l + j * per + l0;
+      x[j] = at < a.n_split && e < a.k ? __ldg(val + at * stride + e) : NAN;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const uint32_t key_x = order_key(x[j]);
+      const bool keep = key_x != 0u && key_x >= least;
+      const uint32_t votes = __ballot_sync(0xffffffffu, keep);
+      const int pos = n + __popc(votes & ((1u << lane) - 1u));
+      // the id is fetched for the few that stay; an unused place of a list is -inf with id -1 and sorts behind
+      if (keep && pos < kMergeCandidates) {
+        const int i = __ldg(id + (l + j * per + l0) * stride + e);
+        cand[pos] = i < 0 ? 0ull : pack_entry(key_x, i);
+      }
+      n += __popc(votes);
+    }
   }
   __syncwarp();
-  constexpr int kLists = 4;                                         // n_split <= 32 * kLists
-  int head[kLists];
-#pragma unroll
-  for (int q = 0; q < kLists; ++q) head[q] = 0;
+  auto put = [&](int at, unsigned long long entry) {
+    a.out_ids[(size_t)t * a.k + at] = entry == 0ull ? -1 : (int)~(uint32_t)entry;
+    a.out_logp[(size_t)t * a.k + at] = a.kappa * (key_value((uint32_t)(entry >> 32)) - M) - ln_s;
+  };
+  if (n <= kMergeCandidates) {
+    for (int c = lane; c < max(n, a.k); c += 32) {
+      if (c >= n) { put(c, 0ull); continue; }                       // fewer than k entries are numbers
+      const unsigned long long mine = cand[c];
+      int rank = 0;
+      for (int o = 0; o < n; ++o) rank += cand[o] > mine ? 1 : 0;
+      if (mine == 0ull) rank = n + 1;                               // an unused place: written below
+      if (rank < a.k) put(rank, mine);
+    }
+    __syncwarp();
+    int used = 0;
+    for (int c = lane; c < n; c += 32) used += cand[c] != 0ull ? 1 : 0;
+    used = __reduce_add_sync(0xffffffffu, used);
+    for (int c = used + lane; c < min(n, a.k); c += 32) put(c, 0ull);
+    return;
+  }
+  // many equal entries: k rounds, each for the best entry below the last one
+  unsigned long long last = ~0ull;
   for (int at = 0; at < a.k; ++at) {
     unsigned long long best = 0ull;
-#pragma unroll
-    for (int q = 0; q < kLists; ++q) {
-      const int sp = lane + 32 * q;
-      if (sp < a.n_split && head[q] < a.k) {
-        const unsigned long long e = mine[sp * a.k + head[q]];
-        best = e > best ? e : best;
-      }
+    for (int l = 0; l < a.n_split; l += per) {
+      const int li = l + l0;
+      if (li >= a.n_split || e >= a.k) continue;
+      const int i = id[li * stride + e];
+      if (i < 0) continue;
+      const unsigned long long x = pack_entry(order_key(val[li * stride + e]), i);
+      if (x < last && x > best) best = x;
     }
-    unsigned long long top = best;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
-      top = other > top ? other : top;
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
+      best = other > best ? other : best;
     }
-    if (top != 0ull && best == top) {
-#pragma unroll
-      for (int q = 0; q < kLists; ++q) {
-        const int sp = lane + 32 * q;
-        if (sp < a.n_split && head[q] < a.k && mine[sp * a.k + head[q]] == top) ++head[q];
-      }
-    }
-    if (lane == 0) {
-      a.out_ids[(size_t)t * a.k + at] = top == 0ull ? -1 : (int)~(uint32_t)top;
-      a.out_logp[(size_t)t * a.k + at] = a.kappa * (key_value((uint32_t)(top >> 32)) - M) - ln_s;
+    last = best;
+    if (lane == 0) put(at, best);
+    if (best == 0ull) {
+      for (int c = at + 1 + lane; c < a.k; c += 32) put(c, 0ull);
+      return;
     }
   }
 }

@@ -318,7 +318,7 @@ static int launch_umma_impl(const CUtensorMap& ma, const CUtensorMap& mb, const 
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(workers * kCta), 1, 1);
-  cfg.blockDim = dim3(kUmmaThreads, 1, 1);
+  cfg.blockDim = dim3(Tr::threads, 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];

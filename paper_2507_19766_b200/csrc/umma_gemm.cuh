@@ -42,7 +42,6 @@ constexpr int kBM = 128;           // accumulator rows (tensor-memory lanes)
 constexpr int kBN = 256;           // accumulator columns
 constexpr int kBK = 64;            // contraction elements per pipeline stage (128 bytes of bf16)
 constexpr int kUmmaK = 16;         // contraction elements per tcgen05.mma
-constexpr int kUmmaThreads = 192;
 constexpr int kTmemCols = 512;     // two accumulators of kBN columns
 constexpr uint32_t kABytes = kBM * kBK * 2;
 constexpr uint32_t kBBytes = kBN * kBK * 2;
@@ -78,6 +77,9 @@ struct ModeTraits {
   static constexpr int top = kMode == kModeScoresTop8 ? 8 : (kMode == kModeScoresTop32 ? 32 : 0);
   static constexpr bool a_mn = dw;
   static constexpr bool b_mn = dh || dw;
+  static constexpr bool wide = scores || kMode == kModeDistill;       // eight epilogue warps
+  static constexpr int epi_warps = wide ? 8 : 4;
+  static constexpr int threads = 64 + 32 * epi_warps;
   static constexpr int timing_kind = sweep ? 0 : (dz ? 1 : (dh ? 2 : 3));
 };
 
@@ -126,11 +128,13 @@ struct UmmaArgs {
   int l2_a, l2_b;           // ptx::L2Hint of the loads of A and of B (CTA-pair kernels)
   const int* dyn_rows;      // optional device count of rows of the whole (compacted) batch: the launch then
   int dyn_base;             // covers rows [dyn_base, min(dyn_base + capacity, *dyn_rows)) of it (M, or K for d_W)
-  // kModeScores*: partials hold (m, r, u, -), m the maximum of the raw accumulators a, r = sum 2^(c2 (a - m)) without
-  // the maximum's own 1, u = sum 2^(c2 (a - m)) c2 (a - m); targets may be NULL
+  // kModeScores*, kModeDistill: partials hold (m, r, u, -), m the maximum of the raw accumulators a, r = sum
+  // 2^(c2 (a - m)) without the maximum's own 1, u = sum 2^(c2 (a - m)) c2 (a - m); two of them per split, of the left and
+  // of the right halves of its tiles.  kModeScores*: targets may be NULL
   int top_k;                // entries of a row's list that are written
-  float* top_val;           // [n_split][T_total][top_k] raw accumulators, falling; -inf where there are fewer
-  int* top_id;              // [n_split][T_total][top_k]; -1 where there are fewer
+  float* top_val;           // [2 n_split][T_total][top_k] raw accumulators, falling; -inf where there are fewer
+  int* top_id;              // [2 n_split][T_total][top_k]; -1 where there are fewer
+  uint32_t* top_pub;        // [min(2 n_split, 32)][T_total], zero before the launch
   // kModeDistill
   int list_k;               // slots of a row's list
   const int* list_ids;      // [T_total][list_k] distinct ids in rising order, then INT_MAX
@@ -223,109 +227,28 @@ __device__ __forceinline__ void stats_chunk(const uint32_t (&raw)[32], int nvali
   run_u += u0 + u1;
 }
 
-// raw[idx] = -inf, likewise for an index only known at run time.
+// The same by five levels of selects on the bits of idx: 31 instructions in five dependent steps instead of a
+// chain of 32 (the chain needs no predicate registers beyond one, which the code around it may need).
+__device__ __forceinline__ float pick_by_bits(const uint32_t (&raw)[32], int idx) {
+  uint32_t a[16], b[8], c[4], d[2];
+  const bool p4 = idx & 16, p3 = idx & 8, p2 = idx & 4, p1 = idx & 2, p0 = idx & 1;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) a[j] = p4 ? raw[j + 16] : raw[j];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b[j] = p3 ? a[j + 8] : a[j];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c[j] = p2 ? b[j + 4] : b[j];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) d[j] = p1 ? c[j + 2] : c[j];
+  return __uint_as_float(p0 ? d[1] : d[0]);
+}
+
+// raw[idx] = -1e30 (kNoColumn), likewise for an index only known at run time.
 __device__ __forceinline__ void drop_column(uint32_t (&raw)[32], int idx) {
 #pragma unroll
   for (int j = 0; j < 32; ++j)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, 0fFF800000;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, 0fF149F2CA;\n\t}"
                  : "+r"(raw[j]) : "r"(idx), "r"(j));
-}
-
-// One 32-column chunk of a row folded into (m, r, u): m the maximum so far, r the sum of 2^(c2 (a - m)) over all
-// entries but ONE that equals m, u = sum 2^(c2 (a - m)) c2 (a - m).  Leaving the maximum's own 1 out keeps the
-// relative precision of 1 - p and of the entropy in sharply peaked rows, where r is 10^-6 and would lose
-// most of its digits beside a one.  The branch on a new maximum is taken a few times per row (harmonic in the
-// number of chunks).  Entries of -inf (dropped ones) count nothing; kEnt = false leaves u alone.
-template <bool kFull, bool kEnt>
-__device__ __forceinline__ void rest_chunk(const uint32_t (&raw)[32], int nvalid, float c2, float& m, float& r, float& u) {
-  float cmax = -INFINITY;
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (kFull || j < nvalid) cmax = fmaxf(cmax, __uint_as_float(raw[j]));
-  float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
-  if (cmax > m) {
-    if (m > -INFINITY) {
-      const float d = fmaxf((m - cmax) * c2, -1000.f), sc = ex2f(d);
-      if (kEnt) u = sc * fmaf(d, r + 1.f, u);
-      r = (r + 1.f) * sc;
-    }
-    m = cmax;
-    float ties = -1.f;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      if (kFull || j < nvalid) {
-        const float t = (__uint_as_float(raw[j]) - m) * c2;
-        const float e = ex2f(t);
-        const bool top = __uint_as_float(raw[j]) == m;
-        ties += top ? 1.f : 0.f;
-        s0 += top ? 0.f : e;
-        if (kEnt) u0 = fmaf(e, t, u0);
-      }
-    }
-    r += s0 + ties;
-    if (kEnt) u += u0;
-    return;
-  }
-  if (!kEnt && m == -INFINITY) return;                 // nothing but dropped entries so far
-#pragma unroll
-  for (int j = 0; j < 32; j += 2) {
-    if (kFull || j < nvalid) {
-      const float t = (__uint_as_float(raw[j]) - m) * c2;
-      const float e = ex2f(t);
-      s0 += e;
-      if (kEnt) u0 = fmaf(e, t, u0);
-    }
-    if (kFull || j + 1 < nvalid) {
-      const float t = (__uint_as_float(raw[j + 1]) - m) * c2;
-      const float e = ex2f(t);
-      s1 += e;
-      if (kEnt) u1 = fmaf(e, t, u1);
-    }
-  }
-  r += s0 + s1;
-  if (kEnt) u += u0 + u1;
-}
-
-// The kTop largest entries of a row seen so far, falling; equal values in the order they came (columns are swept in
-// rising order, so ties go to the lower id).  All indices are static, so the list stays in registers.
-template <int kTop>
-struct TopList {
-  float val[kTop];
-  int id[kTop];
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int j = 0; j < kTop; ++j) { val[j] = -INFINITY; id[j] = -1; }
-  }
-  __device__ __forceinline__ void insert(float x, int i) {
-#pragma unroll
-    for (int j = kTop - 1; j >= 0; --j) {
-      const bool here = x > val[j];                    // x belongs at j or further up
-      const bool up = j > 0 && x > val[j > 0 ? j - 1 : 0];
-      val[j] = up ? val[j > 0 ? j - 1 : 0] : (here ? x : val[j]);
-      id[j] = up ? id[j > 0 ? j - 1 : 0] : (here ? i : id[j]);
-    }
-  }
-};
-template <>
-struct TopList<0> {
-  __device__ __forceinline__ void clear() {}
-};
-
-// The entries of one chunk that beat the list's last one are taken out of the chunk one by one.  A row of N
-// entries in random order has about k (1 + ln(N / k)) of them, so most chunks only pay the comparison.
-template <int kTop>
-__device__ __forceinline__ void top_chunk(const uint32_t (&raw)[32], int nvalid, int col0, TopList<kTop>& list) {
-  uint32_t hits = 0u;
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    hits |= (__uint_as_float(raw[j]) > list.val[kTop - 1]) ? (1u << j) : 0u;
-  if (nvalid < 32) hits &= (1u << nvalid) - 1u;
-  while (hits) {
-    const int j = __ffs(hits) - 1;
-    hits &= hits - 1u;
-    const float x = pick_column(raw, j);
-    if (x > list.val[kTop - 1]) list.insert(x, col0 + j);
-  }
 }
 
 // One 32-column chunk of dz = 2^L (alpha + beta L), L = c2 (a - m) - log2 s; zero at or beyond nvalid, and for a
@@ -379,6 +302,364 @@ __device__ __forceinline__ void put_bf16(uint32_t (&packed)[32], int idx, uint32
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// Epilogue of kModeScores* and kModeDistill: eight warps, two per quarter of the accumulator's rows, one taking
+// the left and one the right half of a tile's columns (each has its own statistics and list of a row, merged
+// afterwards like those of further vocabulary splits).  An element costs one exponential, and that unit gives a
+// warp 32 results in eight cycles, 256 cycles a chunk of 32 columns; what else a chunk needs is kept below it with
+// packed two-element arithmetic, and the second warp runs while the first waits for tensor memory or a branch.
+// With four warps and scalar arithmetic a tile of 256 x 256 took 13400 cycles (8192 tokens x 32768 entries, H 512:
+// 393 us), more than its contraction up to H = 1600.
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
+      "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// Stands for a column that does not count (beyond the vocabulary, or on a teacher's list): its exponential is zero
+// and, unlike that of -inf, so is the product with its exponent.
+constexpr float kNoColumn = -1e30f;
+
+// Running statistics of a row: m the maximum of the raw accumulators, r = sum 2^(c2 a - ref) over all entries but ONE
+// that equals m, u = sum 2^(c2 a - ref) (c2 a - ref).  Leaving the maximum's own 1 out keeps the relative precision of
+// 1 - p and of the entropy in sharply peaked rows, where r is 10^-6 and would lose most of its digits beside a one.
+// ref is c2 m rounded, so that an exponent is one fused multiply-add; delta is what the rounding took off, and
+// finish() puts it back.
+struct RestSums {
+  float m = -INFINITY, ref = 0.f, delta = 0.f, r = 0.f, u = 0.f;
+
+  // `raw` holds 32 numbers (kNoColumn among them), cmax their maximum
+  template <bool kEnt>
+  __device__ __forceinline__ void fold(const uint32_t (&raw)[32], float cmax, float c2) {
+    const bool risen = cmax > m;
+    if (risen) {                                       // a few times per row: harmonic in the number of chunks
+      const float ref_new = c2 * cmax;
+      if (m > -INFINITY) {
+        const float d = fmaxf(ref - ref_new, -1000.f), sc = ex2f(d);
+        const float one = fmaf(delta, 0.6931471805599453f, 1.f);
+        if (kEnt) u = sc * (fmaf(d, r + one, u) + delta);
+        r = (r + one) * sc;
+      }
+      m = cmax;
+      ref = ref_new;
+      delta = fmaf(c2, cmax, -ref_new);
+    }
+    float2 s[4] = {}, v[4] = {};                       // independent chains: two warps a scheduler hide little latency
+    const float2 cc = make_float2(c2, c2), nref = make_float2(-ref, -ref);
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float2 t = fma2(make_float2(__uint_as_float(raw[j + 2 * q]), __uint_as_float(raw[j + 2 * q + 1])), cc, nref);
+        const float2 e = make_float2(ex2f(t.x), ex2f(t.y));
+        s[q] = add2(s[q], e);
+        if (kEnt) v[q] = fma2(e, t, v[q]);
+      }
+    }
+    s[0] = add2(add2(s[0], s[1]), add2(s[2], s[3]));
+    float sum = s[0].x + s[0].y;
+    if (risen) {
+      // The new maximum's own 1 is in the sum.  Where the others are at least a quarter of it, taking it off costs
+      // two of the chunk's 24 bits; where they are less the row may be a peaked one, and they are added without it.
+      sum -= fmaf(delta, 0.6931471805599453f, 1.f);
+      if (sum < 0.25f) {
+        sum = -1.f;                                    // of the entries equal to m one does not count
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float a = __uint_as_float(raw[j]);
+          sum += a == m ? 1.f : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float a = __uint_as_float(raw[j]);
+          sum += a == m ? 0.f : ex2f(fmaf(a, c2, -ref));
+        }
+      }
+    }
+    r += sum;
+    if (kEnt) {
+      v[0] = add2(add2(v[0], v[1]), add2(v[2], v[3]));
+      u += (v[0].x + v[0].y) - (risen ? delta : 0.f);
+    }
+  }
+  // (m, r, u) relative to c2 m itself; a row of nothing but columns that do not count is (-inf, 0, 0)
+  __device__ __forceinline__ float4 finish(bool any) const {
+    if (!any) return make_float4(-INFINITY, r != r ? r : 0.f, 0.f, 0.f);
+    const float f = fmaf(-delta, 0.6931471805599453f, 1.f);
+    return make_float4(m, r * f, fmaf(-delta, r, u) * f, 0.f);
+  }
+};
+
+// The kTop largest entries of a row seen so far, falling; equal values in the order they came (columns are swept in
+// rising order, so ties go to the lower id).  All indices are static, so the list stays in registers.  Entries that
+// beat its last one wait in a queue of kQueue slots in shared memory and are inserted together when some
+// lane's queue is full: a warp then pays for the most entries of a lane over many chunks, not in every chunk.
+constexpr int kQueue = 16;
+constexpr int kNoted = 4;
+template <int kTop>
+struct TopList {
+  float val[kTop];
+  int id[kTop];
+  float best[kNoted];                                  // the largest group maxima, falling
+  float bar;                                           // entries that do not exceed it are not wanted
+  uint32_t queue, next;                                // shared-memory addresses of the lane's first and next free slot
+  static constexpr uint32_t kSlot = 2048;              // bytes from a lane's slot to its next one (256 lanes x 8)
+  __device__ __forceinline__ void clear(bool live) {
+#pragma unroll
+    for (int j = 0; j < kTop; ++j) { val[j] = -INFINITY; id[j] = -1; }
+#pragma unroll
+    for (int j = 0; j < kNoted; ++j) best[j] = -INFINITY;
+    bar = live ? kNoColumn : INFINITY;
+    next = queue;
+  }
+  __device__ __forceinline__ void insert(float x, int i) {
+    bool above[kTop];
+#pragma unroll
+    for (int j = 0; j < kTop; ++j) above[j] = x > val[j];
+#pragma unroll
+    for (int j = kTop - 1; j > 0; --j) {
+      val[j] = above[j - 1] ? val[j - 1] : (above[j] ? x : val[j]);
+      id[j] = above[j - 1] ? id[j - 1] : (above[j] ? i : id[j]);
+    }
+    val[0] = above[0] ? x : val[0];
+    id[0] = above[0] ? i : id[0];
+  }
+  // Notes a group's maximum for what the row's lists publish (see wide_sweep).
+  __device__ __forceinline__ void note(float x) {
+#pragma unroll
+    for (int j = 0; j < kNoted; ++j) {
+      const float hi = fmaxf(best[j], x);
+      x = fminf(best[j], x);
+      best[j] = hi;
+    }
+  }
+  // best[q] for a q only known at run time (see pick_column)
+  __device__ __forceinline__ float noted(int q) const {
+    float v = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kNoted; ++j)
+      asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, %3;\n\t}"
+                   : "+f"(v) : "r"(q), "r"(j), "f"(best[j]));
+    return v;
+  }
+  __device__ __forceinline__ void flush() {            // the whole warp
+    const uint32_t end = queue + __reduce_max_sync(0xffffffffu, next - queue);
+    for (uint32_t at = queue; at < end; at += kSlot) {
+      float x = -INFINITY;
+      int i = 0;
+      if (at < next) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=f"(x), "=r"(i) : "r"(at) : "memory");
+      if (__any_sync(0xffffffffu, x > bar)) insert(x > bar ? x : -INFINITY, i);
+      bar = fmaxf(bar, val[kTop - 1]);
+    }
+    next = queue;
+  }
+  // One chunk, all lanes of a warp together.  A group of eight columns is looked at only where some lane's group
+  // maximum is wanted; what it holds goes to the queues in straight-line code.
+  __device__ __forceinline__ void fold(const uint32_t (&raw)[32], const float (&gmax)[4], float cmax, int col0, bool note_it) {
+    if (!__any_sync(0xffffffffu, cmax > bar)) return;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (!__any_sync(0xffffffffu, gmax[g] > bar)) continue;
+      if (__any_sync(0xffffffffu, next > queue + (kQueue - 8) * kSlot)) flush();
+      if (note_it) note(gmax[g]);
+#pragma unroll
+      for (int j = 8 * g; j < 8 * g + 8; ++j)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %1, %2;\n\t@p st.shared.v2.b32 [%0], {%1, %3};\n\t@p add.u32 %0, %0, 2048;\n\t}"
+                     : "+r"(next) : "f"(__uint_as_float(raw[j])), "f"(bar), "r"(col0 + j) : "memory");
+    }
+  }
+};
+template <>
+struct TopList<0> {};
+
+// Keys in the order of the values, for a word that several SMs write and read while they run; -inf is 0, "none".
+__device__ __forceinline__ void publish_key(uint32_t* at, float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  const uint32_t key = x > -INFINITY ? ((b & 0x80000000u) ? ~b : (b | 0x80000000u)) : 0u;
+  asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(at), "r"(key) : "memory");
+}
+__device__ __forceinline__ uint32_t read_key(const uint32_t* at) {
+  uint32_t key;
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(key) : "l"(at) : "memory");
+  return key;
+}
+// The least of n keys that lie `stride` words apart.
+__device__ __forceinline__ uint32_t least_key(const uint32_t* at, int n, int stride) {
+  uint32_t least = 0xFFFFFFFFu;
+  int j = 0;
+  for (; j + 8 <= n; j += 8) {
+    uint32_t key[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) key[q] = read_key(at + (size_t)(j + q) * stride);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) least = min(least, key[q]);
+  }
+  for (; j < n; ++j) least = min(least, read_key(at + (size_t)j * stride));
+  return least;
+}
+// Maximum of the chunk's columns [8 g, 8 g + 8).
+__device__ __forceinline__ float max_of_group(const uint32_t (&raw)[32], int g) {
+  float m = __uint_as_float(raw[8 * g]);
+#pragma unroll
+  for (int j = 1; j < 8; ++j) m = fmaxf(m, __uint_as_float(raw[8 * g + j]));
+  return m;
+}
+// The largest value below the one with this key; below zero that is a subnormal, not -0, which compares equal to it.
+__device__ __forceinline__ float value_below(uint32_t key) {
+  const uint32_t k = key == 0x80000000u ? key - 2u : key - 1u;
+  return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
+}
+
+template <int kMode, int kCta>
+__device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int n_workers, int n_units, int cta_rank,
+                                           uint32_t queues, uint32_t tmem_base, uint32_t bar_full, uint32_t bar_empty,
+                                           volatile int* abort_p) {
+  using namespace ptx;
+  using Tr = ModeTraits<kMode>;
+  constexpr bool kEnt = Tr::scores;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int quarter = warp & 3;                       // tensor-memory lanes 32 * quarter ..
+  const int half = (warp - 2) >> 2;                   // columns 128 * half .. of a tile
+  const float c2 = args.kappa * 1.4426950408889634f;
+  [[maybe_unused]] TopList<Tr::top> list;
+  if constexpr (Tr::top > 0) list.queue = queues + (threadIdx.x - 64) * 8;
+  uint32_t acc_iter = 0;
+  for (int unit = worker; unit < n_units; unit += n_workers) {
+    const int m_tile = unit / args.n_split, split = unit % args.n_split;
+    int n_begin, n_end;
+    stats_tile_range(args, split, n_begin, n_end);
+    const int row = (m_tile * kCta + cta_rank) * kBM + quarter * 32 + lane;
+    const bool row_ok = row < args.M;
+    const int grow = args.row0 + row;
+    RestSums sums;
+    bool any = false;
+    int y = -1;
+    if (Tr::scores && row_ok && args.targets != nullptr) {
+      y = args.targets[grow];
+      if (y < 0 || y >= args.N) {
+        atomicOr(args.status, kStatusBadTarget);
+        y = y < 0 ? 0 : args.N - 1;
+      }
+    }
+    // What the row's lists have seen bounds its top from below: where each of n of them has q entries of x or more,
+    // n q >= top_k, the row has top_k.  Every list publishes its q-th largest group maximum (as an ordered key, 0 for
+    // none) and takes the least of the n published ones, once per tile; in a unit's first tile the accumulators are read
+    // once for their group maxima before they are read for their entries.  Lists of one row run side by side, so nearly
+    // all entries that are only large for their own split stay out: with 18 lists of 8448 columns each and k = 32 a
+    // list sees about 20 instead of 210.  The keys only rise and an entry of the row's top is never below them,
+    // so what the merge picks does not depend on when they are read.  (Few, long lists: q > kNoted, nothing published.)
+    [[maybe_unused]] const int n_pub = min(2 * args.n_split, 32), q_pub = (args.top_k + n_pub - 1) / n_pub;
+    if constexpr (Tr::top > 0) list.clear(row_ok);
+    [[maybe_unused]] int pos = 0, next_id = INT_MAX;  // kModeDistill: the next id of the row's list in this sweep
+    [[maybe_unused]] const int* ids = nullptr;
+    if (kMode == kModeDistill && row_ok) {
+      ids = args.list_ids + (size_t)grow * args.list_k;
+      int hi = args.list_k;
+      while (pos < hi) {                              // first id at or behind the split's first column
+        const int mid = (pos + hi) >> 1;
+        if (ids[mid] < n_begin * kBN) pos = mid + 1; else hi = mid;
+      }
+      if (pos < args.list_k) next_id = ids[pos];
+    }
+    for (int n_tile = n_begin; n_tile < n_end; ++n_tile, ++acc_iter) {
+      const uint32_t buf = acc_iter & 1u, buf_phase = (acc_iter >> 1) & 1u;
+      // the warp gives up together: its tensor-memory loads are collective
+      const bool ok = mbar_wait_bounded<true>(bar_full + buf * (uint32_t)sizeof(uint64_t), buf_phase, abort_p, kWaitLimitCycles);
+      if (!__all_sync(0xffffffffu, ok)) return;
+      tc_fence_after_sync();
+      const uint32_t taddr = tmem_base + buf * kBN + half * 128 + ((uint32_t)(quarter * 32) << 16);
+      const int first = n_tile * kBN + half * 128;
+      if constexpr (Tr::top > 0) {
+        if (q_pub <= kNoted) {
+          if (n_tile == n_begin) {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              const int col0 = first + c * 32;
+              if (col0 + 32 > args.N) break;          // a ragged chunk is left out of the bound
+              uint32_t raw[32];
+              tmem_ld_32x32(taddr + c * 32, raw);
+              tmem_ld_wait();
+#pragma unroll
+              for (int g = 0; g < 4; ++g) list.note(max_of_group(raw, g));
+            }
+          }
+          if (row_ok) {
+            uint32_t* pub = args.top_pub + grow;
+            const bool mine = 2 * split + half < n_pub;
+            if (mine) publish_key(pub + (size_t)(2 * split + half) * args.T_total, list.noted(q_pub - 1));
+            const uint32_t least = least_key(pub, n_pub, args.T_total);
+            // entries that equal the bound may be needed (the lower id wins), those below it are not
+            if (least != 0u) list.bar = fmaxf(list.bar, value_below(least));
+          }
+          __syncwarp();
+        }
+      }
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        const int col0 = first + c * 32;
+        if (col0 >= args.N) break;
+        const int nvalid = min(32, args.N - col0);
+        uint32_t raw[32];
+        tmem_ld_32x32(taddr + c * 32, raw);
+        tmem_ld_wait();
+        if (nvalid < 32) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) raw[j] = j < nvalid ? raw[j] : __float_as_uint(kNoColumn);
+        }
+        if constexpr (kMode == kModeDistill) {
+          while (next_id < col0 + 32) {               // INT_MAX: no more ids, or no row
+            if (next_id >= col0) {                    // else the other half's
+              args.list_z[(size_t)grow * args.list_k + pos] = pick_by_bits(raw, next_id - col0);
+              drop_column(raw, next_id - col0);
+            }
+            ++pos;
+            next_id = pos < args.list_k ? ids[pos] : INT_MAX;
+          }
+          __syncwarp();                               // the next tensor-memory load is the whole warp's
+        }
+        float gmax[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) gmax[g] = max_of_group(raw, g);
+        const float cmax = fmaxf(fmaxf(gmax[0], gmax[1]), fmaxf(gmax[2], gmax[3]));
+        if (kMode == kModeDistill) any = any || cmax > kNoColumn;
+        sums.fold<kEnt>(raw, cmax, c2);
+        if constexpr (Tr::top > 0) {
+          list.fold(raw, gmax, cmax, col0, n_tile > n_begin);
+        }
+        if (Tr::scores && y >= col0 && y < col0 + 32) args.acc_y[grow] = pick_by_bits(raw, y - col0);
+        __syncwarp();
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        const uint32_t bar = bar_empty + buf * (uint32_t)sizeof(uint64_t);
+        if (kCta == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
+        else mbar_arrive(bar);
+      }
+    }
+    const size_t at = (size_t)(2 * split + half) * args.T_total + grow;
+    if constexpr (Tr::top > 0) {
+      list.flush();
+      if (row_ok) {
+#pragma unroll
+        for (int j = 0; j < Tr::top; ++j)
+          if (j < args.top_k) { args.top_val[at * args.top_k + j] = list.val[j]; args.top_id[at * args.top_k + j] = list.id[j]; }
+      }
+    }
+    if (row_ok) args.partials[at] = sums.finish(kMode == kModeDistill ? any : sums.m > -INFINITY);
+  }
+}
+
 // kModeDHiddenPart: unit -> output tile and the k-blocks of its part (every part has some); else all k-blocks.
 template <int kMode>
 __device__ __forceinline__ int part_of_unit(int unit, int k_blocks, const UmmaArgs& args, int& kb_begin, int& kb_end) {
@@ -390,7 +671,7 @@ __device__ __forceinline__ int part_of_unit(int unit, int k_blocks, const UmmaAr
 }
 
 template <int kMode, int kCta, int kAcc>
-__global__ void __launch_bounds__(kUmmaThreads, 1)
+__global__ void __launch_bounds__(ModeTraits<kMode>::threads, 1)
 umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
             const __grid_constant__ CUtensorMap map_c, const UmmaArgs args_in) {
   using namespace ptx;
@@ -446,7 +727,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
     for (int b = 0; b < 2; ++b) {   // with kAcc = 2 only entry 0 is used
       mbar_init(smem_u32(&bar_tmem_full[b]), 1);
-      mbar_init(smem_u32(&bar_tmem_empty[b]), 4 * kCta);   // one arrival per epilogue warp of every CTA
+      mbar_init(smem_u32(&bar_tmem_empty[b]), Tr::epi_warps * kCta);   // one arrival per epilogue warp of every CTA
     }
     mbar_fence_init();
     fence_async_proxy();
@@ -641,6 +922,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     mma_done:;
     }
     __syncwarp();
+  } else if constexpr (Tr::wide) {
+    wide_sweep<kMode, kCta>(args, worker, n_workers, n_units, cta_rank, smem_base + kStagesT * kStageBytesCta, tmem_base,
+                            smem_u32(&bar_tmem_full[0]), smem_u32(&bar_tmem_empty[0]), abort_p);
   } else {
     // ------------------------------------------------------------------ epilogue (warps 2..5, every CTA)
     const int quarter = warp & 3;                       // tensor-memory lanes 32 * quarter ..
@@ -672,11 +956,11 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       float run_m = -INFINITY, run_s = 0.f, run_u = 0.f;
       int y = -1;
       float coef = 0.f, lse2 = 0.f;
-      if (kMode == kModeStats || kMode == kModeDz || ((Tr::scores || kMode == kModeDzRow) && args.targets != nullptr)) {
+      if (kMode == kModeStats || kMode == kModeDz || (kMode == kModeDzRow && args.targets != nullptr)) {
         if (row_ok) {
           y = args.targets[grow];
           if (y < 0 || y >= args.N) {
-            if (Tr::sweep) atomicOr(args.status, kStatusBadTarget);
+            if (kMode == kModeStats) atomicOr(args.status, kStatusBadTarget);
             y = y < 0 ? 0 : args.N - 1;
           }
         }
@@ -684,18 +968,6 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       if (kMode == kModeStats && args.resume && row_ok) {  // continue the sweep the launch before left off
         const float4 p = args.partials[(size_t)split * args.T_total + grow];
         run_m = p.x; run_s = p.y; run_u = p.z;
-      }
-      [[maybe_unused]] TopList<Tr::top> list;
-      if constexpr (Tr::top > 0) list.clear();
-      [[maybe_unused]] int list_pos = 0, next_id = INT_MAX;   // kModeDistill: the next id of the row's list in this sweep
-      if (kMode == kModeDistill && row_ok) {
-        const int* ids = args.list_ids + (size_t)grow * args.list_k;
-        int hi = args.list_k;
-        while (list_pos < hi) {                               // first id at or behind the split's first column
-          const int mid = (list_pos + hi) >> 1;
-          if (ids[mid] < n_begin * kUnitN) list_pos = mid + 1; else hi = mid;
-        }
-        if (list_pos < args.list_k) next_id = ids[list_pos];
       }
       [[maybe_unused]] float4 rp = make_float4(0.f, 0.f, 0.f, 0.f);   // kModeDzRow
       [[maybe_unused]] float ins = 0.f;
@@ -808,24 +1080,6 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             if (row_ok && y >= col0 && y < col0 + 32) {
               args.acc_y[grow] = pick_column(raw, y - col0);
             }
-          } else if constexpr (Tr::scores) {
-            if (nvalid >= 32) rest_chunk<true, true>(raw, 32, c2, run_m, run_s, run_u);
-            else rest_chunk<false, true>(raw, nvalid, c2, run_m, run_s, run_u);
-            if constexpr (Tr::top > 0) {
-              if (row_ok) top_chunk<Tr::top>(raw, nvalid, col0, list);
-              __syncwarp();                                      // the next tensor-memory load is the whole warp's
-            }
-            if (row_ok && y >= col0 && y < col0 + 32) args.acc_y[grow] = pick_column(raw, y - col0);
-          } else if constexpr (kMode == kModeDistill) {
-            while (next_id < col0 + 32) {                        // INT_MAX: no more ids, or no row
-              args.list_z[(size_t)grow * args.list_k + list_pos] = pick_column(raw, next_id - col0);
-              drop_column(raw, next_id - col0);
-              ++list_pos;
-              next_id = list_pos < args.list_k ? args.list_ids[(size_t)grow * args.list_k + list_pos] : INT_MAX;
-            }
-            __syncwarp();                                        // the next tensor-memory load is the whole warp's
-            if (nvalid >= 32) rest_chunk<true, false>(raw, 32, c2, run_m, run_s, run_u);
-            else rest_chunk<false, false>(raw, nvalid, c2, run_m, run_s, run_u);
           } else if (kMode == kModeDHidden) {
             if (row_ok) {
               uint32_t packed[16];
@@ -875,16 +1129,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         }
       }
 
-      if constexpr (Tr::top > 0) {
-        if (row_ok) {
-          float* tv = args.top_val + ((size_t)split * args.T_total + grow) * args.top_k;
-          int* ti = args.top_id + ((size_t)split * args.T_total + grow) * args.top_k;
-#pragma unroll
-          for (int j = 0; j < Tr::top; ++j)
-            if (j < args.top_k) { tv[j] = list.val[j]; ti[j] = list.id[j]; }
-        }
-      }
-      if (Tr::sweep && row_ok)
+      if (kMode == kModeStats && row_ok)
         args.partials[(size_t)split * args.T_total + grow] = make_float4(run_m, run_s, run_u, 0.f);
     }
   }
