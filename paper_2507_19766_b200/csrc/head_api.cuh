@@ -2,6 +2,7 @@
 #pragma once
 
 #include "scores.cuh"
+#include "small_batch.cuh"
 
 namespace ulorl {
 
@@ -9,16 +10,17 @@ constexpr int kHeadMaxSplits = kMaxRowLists / 2;   // a split leaves two partial
 
 struct HeadPlan {
   bool tensor;
+  bool small;                              // tensor path, few tokens: the forward calls go through a panel of logits
   int sms, workers;                        // workers: CTA pairs
   int n_split, tiles_per_split;            // vocabulary splits of the forward sweep
   int n_partial;                           // partial results of a row that it leaves
   int panel_tokens, n_panels;
-  size_t dz_ld;
+  size_t dz_ld, logits_ld;
   bool dw_direct;                          // d_W leaves the contraction as bf16: one panel, nothing to add to
   bool dw_acc;                             // d_W summed in float32 in the workspace, rounded at the end
   int dh_parts, dh_part_blocks, dh_part_rows;
   // forward scratch
-  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_top_pub, off_sorted, off_slots, off_list_z, fwd_total;
+  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_top_pub, off_sorted, off_slots, off_list_z, off_logits, fwd_total;
   // backward scratch, over the same bytes
   size_t off_row_p, off_row_ins, off_panel, off_dw_acc, off_parts, bwd_total;
 };
@@ -51,13 +53,14 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   pl.sms = device_sm_count();
   pl.workers = std::max(1, pl.sms / 2);
   const int T = p->T, V = p->V, H = p->H;
+  pl.small = pl.tensor && T <= kSmallMaxTokens;
   const size_t T1 = (size_t)std::max(T, 1), K = (size_t)p->top_k;
   const int tile_m = 2 * kBM;
   const int m_tiles = std::max(1, (T + tile_m - 1) / tile_m);
   const int n_tiles = (V + kBN - 1) / kBN;
   pl.n_split = 1;
   pl.tiles_per_split = n_tiles;
-  if (pl.tensor) {
+  if (pl.tensor && !pl.small) {
     // As for the policy loss: enough splits that the live hidden tiles stay in L2, then the count with the shortest
     // modelled time, waves of units x time of a unit, the fewest splits within one percent.  A unit's time is that
     // of its contractions (8 H cycles a tile) or that of its epilogue, whichever is longer: about 2400 cycles a tile
@@ -84,7 +87,7 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
     pl.tiles_per_split = (n_tiles + want - 1) / want;
     pl.n_split = (n_tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
   }
-  pl.n_partial = pl.tensor ? 2 * pl.n_split : 1;
+  pl.n_partial = pl.tensor && !pl.small ? 2 * pl.n_split : 1;
   // backward panels
   int panel = p->bwd_panel_tokens > 0 ? p->bwd_panel_tokens : (pl.tensor ? pl.workers * tile_m : kDefaultPanelSimt);
   if (!pl.tensor) panel = std::min(panel, 32768);                   // rows are a grid dimension there
@@ -92,7 +95,8 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   panel = (int)std::min<long>((long)align_up((size_t)panel, (size_t)unit), (long)align_up(T1, (size_t)unit));
   pl.panel_tokens = panel;
   pl.n_panels = (int)((T1 + panel - 1) / panel);
-  pl.dz_ld = pl.tensor ? align_up((size_t)V, 64) : (size_t)V;
+  pl.dz_ld = align_up((size_t)V, pl.tensor ? 64 : 4);
+  pl.logits_ld = align_up((size_t)V, 4);
   const bool want_bf16 = p->dw_dtype == ULORL_BF16;
   pl.dw_direct = pl.tensor && want_bf16 && pl.n_panels == 1 && !p->dw_accumulate;
   pl.dw_acc = want_bf16 && !pl.dw_direct;
@@ -118,13 +122,13 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   pl.off_sorted = off;    off = align_up(off + sizeof(int) * T1 * K, 256);
   pl.off_list_z = off;    off = align_up(off + sizeof(float) * T1 * K, 256);
   pl.off_slots = off;     off = align_up(off + T1 * K, 1024);
-  pl.off_panel = off;     // the CUDA-core path's forward pass holds a panel of logits
-  pl.fwd_total = pl.tensor ? off : align_up(off + sizeof(float) * (size_t)panel * pl.dz_ld, 1024);
+  pl.off_logits = off;    // forward passes that go through a panel of logits
+  pl.fwd_total = off;
+  if (pl.small || !pl.tensor) pl.fwd_total = align_up(off + sizeof(float) * (size_t)std::min(panel, (int)T1) * pl.logits_ld, 1024);
   off = 256;
   pl.off_row_p = off;     off = align_up(off + sizeof(float4) * T1, 256);
   pl.off_row_ins = off;   off = align_up(off + sizeof(float) * T1, 1024);
-  if (pl.tensor) pl.off_panel = off;
-  else off = pl.off_panel = std::max(off, pl.off_panel);
+  pl.off_panel = off;
   off = align_up(off + (size_t)panel * pl.dz_ld * (pl.tensor ? 2 : 4), 1024);
   if (pl.dw_acc) { pl.off_dw_acc = off; off = align_up(off + sizeof(float) * (size_t)V * (size_t)H, 1024); }
   if (pl.dh_parts > 1) {
@@ -177,9 +181,86 @@ static int simt_logits_panel(const ulorl_head_params_t* p, const void* hidden, c
   return check_launch();
 }
 
+template <int kN>
+static int launch_small(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, float* logits,
+                        int* status, cudaStream_t stream) {
+  using Cfg = SmallConfig<kN>;
+  static bool opted_in[kMaxDevices] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return ULORL_ERR_CUDA;
+  {
+    std::lock_guard<std::mutex> lock(g_setup_mutex);
+    if (!opted_in[dev]) {
+      if (cudaFuncSetAttribute(small_logits_kernel<kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::smem_bytes) !=
+          cudaSuccess)
+        return ULORL_ERR_CUDA;
+      opted_in[dev] = true;
+    }
+  }
+  SmallArgs a{};
+  a.T = p->T; a.V = p->V; a.K = p->H;
+  a.rows_per_cta = (int)align_up((size_t)(p->V + pl.sms - 1) / pl.sms, 16);
+  a.logits = logits;
+  a.ld = pl.logits_ld;
+  a.status = status;
+  const int last = a.rows_per_cta - (a.rows_per_cta - 1) / kBM * kBM;
+  CUtensorMap map_w, map_last, map_h;
+  int st = make_map_bf16(&map_w, W, (uint64_t)p->V, (uint64_t)p->H, (uint64_t)p->H, kBK, kBM);
+  if (st != ULORL_OK) return st;
+  st = make_map_bf16(&map_last, W, (uint64_t)p->V, (uint64_t)p->H, (uint64_t)p->H, kBK, (uint32_t)last);
+  if (st != ULORL_OK) return st;
+  st = make_map_bf16(&map_h, hidden, (uint64_t)p->T, (uint64_t)p->H, (uint64_t)p->H, kBK, kN);
+  if (st != ULORL_OK) return st;
+  const unsigned blocks = (unsigned)((p->V + a.rows_per_cta - 1) / a.rows_per_cta);
+  small_logits_kernel<kN><<<blocks, kSmallThreads, Cfg::smem_bytes, stream>>>(map_w, map_last, map_h, a);
+  return check_launch();
+}
+
+// logits[i, v] = hidden[t0 + i] . W[v] in float32 for the paths that go through a panel of logits.
+static int logits_panel(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, int t0, int rows,
+                        float* logits, uint8_t* ws, cudaStream_t stream) {
+  if (!pl.small)
+    return p->dtype == ULORL_F32 ? simt_logits_panel<float>(p, hidden, W, t0, rows, logits, pl.logits_ld, stream)
+                                 : simt_logits_panel<__nv_bfloat16>(p, hidden, W, t0, rows, logits, pl.logits_ld, stream);
+  int* status = reinterpret_cast<int*>(ws + pl.off_status);
+  if (p->T <= 16) return launch_small<16>(p, pl, hidden, W, logits, status, stream);
+  if (p->T <= 32) return launch_small<32>(p, pl, hidden, W, logits, status, stream);
+  return launch_small<64>(p, pl, hidden, W, logits, status, stream);
+}
+
+// Rows are spread over clusters until there are two blocks a multiprocessor, as long as a block keeps four loads a
+// thread; more than eight blocks a cluster have to be asked for, once per device.
 template <typename T>
-static int launch_rows(const RowsArgs& a, cudaStream_t stream) {
-  logits_rows_kernel<T><<<a.T, kRowThreads, 0, stream>>>(a);
+static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
+  static bool opted_in[kMaxDevices] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return ULORL_ERR_CUDA;
+  {
+    std::lock_guard<std::mutex> lock(g_setup_mutex);
+    if (!opted_in[dev]) {
+      if (cudaFuncSetAttribute(logits_rows_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+        return ULORL_ERR_CUDA;
+      opted_in[dev] = true;
+    }
+  }
+  const int least = kRowThreads * kRowUnroll * RowType<T>::per_vec;
+  int cluster = 1;
+  while (cluster < kRowMaxCluster && (long)a.T * cluster * 2 <= 2L * sms && a.V >= 2 * cluster * least) cluster *= 2;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)a.T * (unsigned)cluster, 1, 1);
+  cfg.blockDim = dim3(kRowThreads, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, logits_rows_kernel<T>, a) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return ULORL_ERR_CUDA;
+  }
   return check_launch();
 }
 
@@ -370,7 +451,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
   st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.fwd_total, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (pl.tensor) {
+  if (pl.tensor && !pl.small) {
     UmmaArgs a{};
     a.targets = logp ? targets : nullptr;
     a.acc_y = reinterpret_cast<float*>(ws + pl.off_acc_y);
@@ -394,14 +475,13 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
     merge_scores_kernel<<<(T + kMergeWarps - 1) / kMergeWarps, 32 * kMergeWarps, 0, stream>>>(m);
     return check_launch();
   }
-  float* panel = reinterpret_cast<float*>(ws + pl.off_panel);
+  float* panel = reinterpret_cast<float*>(ws + pl.off_logits);
   for (int t0 = 0; t0 < T; t0 += pl.panel_tokens) {
     const int rows = std::min(T - t0, pl.panel_tokens);
-    st = params->dtype == ULORL_F32 ? simt_logits_panel<float>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream)
-                                    : simt_logits_panel<__nv_bfloat16>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream);
+    st = logits_panel(params, pl, hidden, W, t0, rows, panel, ws, stream);
     if (st != ULORL_OK) return st;
     RowsArgs a{};
-    a.logits = panel; a.ld = pl.dz_ld;
+    a.logits = panel; a.ld = pl.logits_ld;
     a.T = rows; a.V = V; a.k = k;
     a.kappa = params->inv_temperature;
     a.targets = targets ? targets + t0 : nullptr;
@@ -412,7 +492,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
     a.top_ids = top_ids ? top_ids + (size_t)t0 * k : nullptr;
     a.top_logp = top_logp ? top_logp + (size_t)t0 * k : nullptr;
     a.status = reinterpret_cast<int*>(ws + pl.off_status);
-    st = launch_rows<float>(a, stream);
+    st = launch_rows<float>(a, pl.sms, stream);
     if (st != ULORL_OK) return st;
   }
   return ULORL_OK;
@@ -463,8 +543,9 @@ int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V,
   a.logp = logp; a.entropy = entropy; a.lse = lse;
   a.top_ids = top_ids; a.top_logp = top_logp;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  return dtype == ULORL_F32 ? launch_rows<float>(a, stream)
-                            : (dtype == ULORL_BF16 ? launch_rows<__nv_bfloat16>(a, stream) : launch_rows<__half>(a, stream));
+  const int sms = device_sm_count();
+  return dtype == ULORL_F32 ? launch_rows<float>(a, sms, stream)
+                            : (dtype == ULORL_BF16 ? launch_rows<__nv_bfloat16>(a, sms, stream) : launch_rows<__half>(a, sms, stream));
 }
 
 int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
@@ -492,7 +573,7 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
   const unsigned row_blocks = (unsigned)((T + 7) / 8);              // eight warps, one token each
   distill_sort_kernel<<<row_blocks, 256, 0, stream>>>(T, K, V, teacher_ids, sorted, slots, status);
   ULORL_LAUNCH_CHECK();
-  if (pl.tensor) {
+  if (pl.tensor && !pl.small) {
     UmmaArgs a{};
     a.list_k = K;
     a.list_ids = sorted;
@@ -500,20 +581,19 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
     st = run_sweep(params, pl, kModeDistill, a, hidden, W, ws, stream);
     if (st != ULORL_OK) return st;
   } else {
-    float* panel = reinterpret_cast<float*>(ws + pl.off_panel);
+    float* panel = reinterpret_cast<float*>(ws + pl.off_logits);
     for (int t0 = 0; t0 < T; t0 += pl.panel_tokens) {
       const int rows = std::min(T - t0, pl.panel_tokens);
-      st = params->dtype == ULORL_F32 ? simt_logits_panel<float>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream)
-                                      : simt_logits_panel<__nv_bfloat16>(params, hidden, W, t0, rows, panel, pl.dz_ld, stream);
+      st = logits_panel(params, pl, hidden, W, t0, rows, panel, ws, stream);
       if (st != ULORL_OK) return st;
-      distill_take_kernel<<<(rows + 7) / 8, 256, 0, stream>>>(rows, t0, K, panel, pl.dz_ld, sorted, list_z);
+      distill_take_kernel<<<(rows + 7) / 8, 256, 0, stream>>>(rows, t0, K, panel, pl.logits_ld, sorted, list_z);
       ULORL_LAUNCH_CHECK();
       RowsArgs a{};
-      a.logits = panel; a.ld = pl.dz_ld;
+      a.logits = panel; a.ld = pl.logits_ld;
       a.T = rows; a.V = V;
       a.kappa = params->inv_temperature;
       a.partials = partials + t0;
-      st = launch_rows<float>(a, stream);
+      st = launch_rows<float>(a, pl.sms, stream);
       if (st != ULORL_OK) return st;
     }
   }

@@ -9,6 +9,7 @@
 // ln s = log1p(r), lse = kappa m + ln s.  Ids are chosen by (value falling, id rising).
 #pragma once
 
+#include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <limits.h>
 
@@ -51,31 +52,71 @@ __device__ __forceinline__ unsigned long long pack_entry(uint32_t key, int id) {
   return ((unsigned long long)key << 32) | (uint32_t)~id;          // larger = better: value, then the lower id
 }
 
+// What the row kernel needs of a type: 16-byte vectors of per_vec entries, the bits of an order key that its values
+// use, the largest entry of a vector (NaN aside), and its entries as float32 pairs, nothing below kFloor (see fold).
+constexpr float kFloor = -1e30f;
 template <typename T> struct RowType;
-template <> struct RowType<float> { static constexpr int per_vec = 4, key_bits = 32; };
-template <> struct RowType<__nv_bfloat16> { static constexpr int per_vec = 8, key_bits = 16; };
-template <> struct RowType<__half> { static constexpr int per_vec = 8, key_bits = 19; };   // 8 exponent + 10 mantissa bits + sign
-
-__device__ __forceinline__ void widen(const uint4& v, float (&x)[4], float) {
-  x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-}
-__device__ __forceinline__ void widen(const uint4& v, float (&x)[8], __nv_bfloat16) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+template <> struct RowType<float> {
+  static constexpr int per_vec = 4, key_bits = 32;
+  static constexpr uint32_t neg_inf = 0xFF800000u;
+  static __device__ __forceinline__ float top(const uint4& v) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
-}
-__device__ __forceinline__ void widen(const uint4& v, float (&x)[8], __half) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
+  static __device__ __forceinline__ void entries(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
-}
+  static __device__ __forceinline__ void floored(const uint4& v, float (&x)[4]) {
+    entries(v, x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = max_nan(x[j], kFloor);
+  }
+};
+template <> struct RowType<__nv_bfloat16> {
+  static constexpr int per_vec = 8, key_bits = 16;
+  static constexpr uint32_t neg_inf = 0xFF80FF80u;
+  static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const __nv_bfloat162 m = __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ void entries(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ void floored(const uint4& v, float (&x)[8]) {
+    const __nv_bfloat162 low = __float2bfloat162_rn(kFloor);
+    const __nv_bfloat162 q[4] = {__hmax2_nan(pair(v.x), low), __hmax2_nan(pair(v.y), low), __hmax2_nan(pair(v.z), low),
+                                 __hmax2_nan(pair(v.w), low)};
+    entries(*reinterpret_cast<const uint4*>(q), x);
+  }
+};
+template <> struct RowType<__half> {
+  static constexpr int per_vec = 8, key_bits = 19;                  // sign, 8 exponent and 10 mantissa bits of the float32
+  static constexpr uint32_t neg_inf = 0xFC00FC00u;
+  static __device__ __forceinline__ __half2 pair(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const __half2 m = __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ void entries(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(pair(w[i]));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ void floored(const uint4& v, float (&x)[8]) {
+    entries(v, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = max_nan(x[j], kFloor);
+  }
+};
 __device__ __forceinline__ float row_value(float x) { return x; }
 __device__ __forceinline__ float row_value(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float row_value(__half x) { return __half2float(x); }
@@ -97,113 +138,189 @@ struct RowsArgs {
 constexpr int kRowThreads = 256;
 constexpr int kRowUnroll = 4;          // 16-byte loads a thread has in flight
 constexpr int kRowCandidates = 512;
+constexpr int kRowMaxCluster = 16;
 
-// Running statistics of a row in one lane: m is the warp's maximum, s and u are the lane's sums over its entries
-// relative to m (u in units of log2) without one entry that equals m where own = 1.
+// Running statistics of a row in one lane: m is the warp's maximum, s and u are the lane's sums of 2^t and 2^t t, t =
+// c2 x - ref, over its entries but one that equals m where own = 1.  ref is c2 m rounded, so that an exponent is one
+// fused multiply-add, and delta what the rounding took off.  Entries of -inf are raised to kFloor, where 2^t and
+// 2^t t are zero; that and the product c2 m hold for maxima between -1e29 and 1e30, and a warp whose maximum lies
+// outside (a row of the type's lowest value) takes differences to it instead.
 struct RowState {
-  float m = -INFINITY, s = 0.f, u = 0.f, own = 0.f;
+  float m = -INFINITY, ref = 0.f, delta = 0.f, s = 0.f, u = 0.f, own = 0.f;
   float lane_max = NAN;                                             // no entry yet
 
-  // folds in n entries (absent ones are -inf; `any`: the lane has some); all lanes of a warp together
-  template <int n>
-  __device__ __forceinline__ void fold(const float (&x)[n], float c2, bool any) {
-    float cmax = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < n; ++j) cmax = fmaxf(cmax, x[j]);
+  __device__ __forceinline__ bool plain() const { return m >= -1e29f && m <= 1e30f; }
+  __device__ __forceinline__ float one() const { return fmaf(delta, kLn2, 1.f); }     // 2^delta
+
+  // folds in n entries: cmax is the largest of them, x their values, not below kFloor; `any`: the lane has some.  All lanes
+  // of a warp together.  `exact` gives entry j as it is.
+  template <int n, typename Exact>
+  __device__ __forceinline__ void fold(const float (&x)[n], float cmax, float c2, bool any, Exact exact) {
     if (any) lane_max = fmaxf(lane_max, cmax);
-    float wmax = cmax;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) wmax = fmaxf(wmax, __shfl_xor_sync(0xffffffffu, wmax, o));
-    float ls = 0.f, lu = 0.f;
-    if (wmax > m) {                                                 // the same in all lanes
+    const int ci = __float_as_int(cmax);
+    const int wi = __reduce_max_sync(0xffffffffu, ci ^ ((ci >> 31) & 0x7FFFFFFF));    // ordered as integers
+    const float wmax = __int_as_float(wi ^ ((wi >> 31) & 0x7FFFFFFF));
+    const bool risen = wmax > m;                                    // the same in all lanes
+    if (risen) {
+      const float ref_new = fminf(fmaxf(c2 * wmax, -1e35f), 1e35f);
       if (m > -INFINITY) {
-        const float d = fmaxf((m - wmax) * c2, -1000.f), sc = fast_ex2(d);   // m may be the type's lowest value
-        u = sc * fmaf(d, s + own, u);
-        s = (s + own) * sc;
+        const float d = fmaxf(ref - ref_new, -1000.f), sc = fast_ex2(d), mine = own * one();
+        u = sc * (fmaf(d, s + mine, u) + own * delta);
+        s = (s + mine) * sc;
         own = 0.f;
       }
       m = wmax;
-      float ties = 0.f;
+      ref = ref_new;
+      delta = plain() ? fmaf(c2, m, -ref) : 0.f;
+    }
+    float ls = 0.f, lu = 0.f;
+    if (plain() || m == -INFINITY) {
+      constexpr int kChains = n >= 8 ? 4 : 1;
+      float2 a[kChains] = {}, b[kChains] = {};
+      const float2 cc = make_float2(c2, c2), nref = make_float2(-ref, -ref);
 #pragma unroll
+      for (int j = 0; j < n; j += 2) {
+        const int q = (j / 2) % kChains;
+        const float2 t = fma2(make_float2(x[j], x[j + 1]), cc, nref);
+        const float2 e = make_float2(fast_ex2(t.x), fast_ex2(t.y));
+        a[q] = add2(a[q], e);
+        b[q] = fma2(e, t, b[q]);
+      }
+#pragma unroll
+      for (int q = 1; q < kChains; ++q) { a[0] = add2(a[0], a[q]); b[0] = add2(b[0], b[q]); }
+      ls = a[0].x + a[0].y;
+      lu = b[0].x + b[0].y;
+      if (risen && cmax == m) {
+        // the new maximum's own 1: taken off the sum where the others are a quarter of it or more, else they are added
+        // without it (a peaked row's 1 - p would lose its digits)
+        ls -= one();
+        lu -= delta;
+        own = 1.f;
+        if (ls < 0.25f) {
+          ls = -1.f;
+#pragma unroll
+          for (int j = 0; j < n; ++j) ls += x[j] == m ? 1.f : 0.f;
+#pragma unroll
+          for (int j = 0; j < n; ++j) ls += x[j] == m ? 0.f : fast_ex2(fmaf(x[j], c2, -ref));
+        }
+      }
+    } else {
+      float ties = 0.f;
+#pragma unroll 1
       for (int j = 0; j < n; ++j) {
-        const float t = max_nan((x[j] - m) * c2, -1000.f);          // an entry of -inf: 0 * -1000, not 0 * -inf
-        const float e = fast_ex2(t);
-        const bool top = x[j] == m;
+        const float v = exact(j);
+        const float t = max_nan((v - m) * c2, -1000.f), e = fast_ex2(t);
+        const bool top = risen && v == m;
         ties += top ? 1.f : 0.f;
         ls += top ? 0.f : e;
         lu = fmaf(e, t, lu);
       }
       if (ties > 0.f) { own = 1.f; ls += ties - 1.f; }
-    } else {
-      const float ref = m > -INFINITY ? m : 0.f;
-#pragma unroll
-      for (int j = 0; j < n; ++j) {
-        const float t = max_nan((x[j] - ref) * c2, -1000.f);
-        const float e = fast_ex2(t);
-        ls += e;
-        lu = fmaf(e, t, lu);
-      }
     }
     s += ls;
     u += lu;
   }
 };
 
-// One block per row, one pass over memory: each warp keeps a running maximum for its lanes, each lane its sums
-// relative to it, and its own largest entry.  The k-th largest of the 256 lane maxima bounds the k-th largest
-// entry from below, and entries at or above it sit in lanes whose maximum is: only their few vectors are read again.
+// What the blocks of one row tell each other: maximum, sums relative to it (the maximum's own 1 not in r if owners > 0),
+// and the slice's largest entries in falling order, 0 behind the last.
+struct RowSlice {
+  float m, r, u;
+  int owners;
+  unsigned long long top[kMaxTop];
+};
+
+// Adds (m, s, u) of n maxima that are not in s to the sums relative to M >= m.
+__device__ __forceinline__ void add_slice(float m, float s, float u, int n, float c2, float M, float& r, float& uu, int& owners) {
+  if (m == M) {
+    r += s;
+    uu += u;
+    owners += n;
+  } else if (m > -INFINITY) {
+    const float d = fmaxf((m - M) * c2, -1000.f), sc = fast_ex2(d), tot = s + (float)n;
+    r = fmaf(tot, sc, r);
+    uu = fmaf(sc, fmaf(d, tot, u), uu);
+  } else {
+    r += s;                                                         // nothing, or the NaN that a NaN entry left
+  }
+}
+
+// A row is read once, by one block or, where there are fewer rows than the GPU takes, by a cluster of up to 16 that
+// each take a slice and merge over distributed shared memory: one launch, no workspace.  Each warp keeps a running
+// maximum for its lanes, each lane its sums relative to it, and its own largest entry.  The k-th largest of the block's
+// 256 lane maxima bounds the k-th largest entry of the slice from below, and entries at or above it sit in lanes whose
+// maximum is: only their few vectors are read again.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads)
 logits_rows_kernel(const RowsArgs args) {
-  constexpr int E = RowType<T>::per_vec;
-  constexpr int kShift = 32 - RowType<T>::key_bits;
-  __shared__ float sh_m[kRowThreads / 32], sh_s[kRowThreads / 32], sh_u[kRowThreads / 32];
-  __shared__ int sh_n[kRowThreads / 32];
+  namespace cg = cooperative_groups;
+  using Type = RowType<T>;
+  constexpr int E = Type::per_vec;
+  constexpr int kShift = 32 - Type::key_bits;
+  constexpr int kWarps = kRowThreads / 32;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int n_slice = (int)cluster.num_blocks(), slice = (int)cluster.block_rank();
+  __shared__ float sh_m[kWarps], sh_s[kWarps], sh_u[kWarps];
+  __shared__ int sh_n[kWarps];
+  __shared__ RowSlice sh_mine;
+  __shared__ float all_m[kRowMaxCluster], all_r[kRowMaxCluster], all_u[kRowMaxCluster];
+  __shared__ int all_n[kRowMaxCluster];
   __shared__ float sh_row[2];                                       // m, ln s
   __shared__ unsigned long long cand[kRowCandidates];
   __shared__ int owners[kRowThreads];
-  __shared__ int n_owner, n_cand, sh_scan[kRowThreads / 32 + 1];
+  __shared__ int n_owner, n_cand, sh_scan[kWarps + 1], sh_rank[kMaxTop];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int V = args.V, k = args.k;
-  const int row = blockIdx.x;
+  const int row = blockIdx.x / n_slice;
   const T* base = static_cast<const T*>(args.logits) + (size_t)row * args.ld;
-  // [0, head) and [V - tail, V) are read element by element, the vectors between them start on 16 bytes
+  // [0, head) and [V - tail, V) are read element by element (by the first block), the vectors between them start on 16 bytes
   const int head = min(V, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(base) & 15u)) & 15u) / sizeof(T)));
-  const int nvec = (V - head) / E;
-  const int extras = V - nvec * E;                                  // head + tail < 2 E
-  const uint4* vecs = reinterpret_cast<const uint4*>(base + head);
-  auto extra_id = [&](int i) { return i < head ? i : nvec * E + i; };
+  const int all_vec = (V - head) / E;
+  const int per_slice = (all_vec + n_slice - 1) / n_slice;
+  const int v0 = min(all_vec, slice * per_slice), nvec = min(all_vec - v0, per_slice);
+  const int extras = slice == 0 ? V - all_vec * E : 0;              // head + tail < 2 E
+  const uint4* vecs = reinterpret_cast<const uint4*>(base + head) + v0;
+  const int first_id = head + v0 * E;
+  auto extra_id = [&](int i) { return i < head ? i : all_vec * E + i; };
+  // the slice's entries in the order of their ids: the first block has the head before its vectors and the tail behind
+  const int n_local = nvec * E + extras;
+  auto local_id = [&](int i) {
+    return slice != 0 ? first_id + i : (i < head + nvec * E ? i : all_vec * E + i - nvec * E);
+  };
   const float c2 = args.kappa * kLog2e;
 
   RowState st;
-
-  {
-    float x[1] = {-INFINITY};
-    if (tid < extras) x[0] = row_value(base[extra_id(tid)]);
-    st.fold<1>(x, c2, tid < extras);
+  if (slice == 0) {
+    const float v = tid < extras ? row_value(base[extra_id(tid)]) : -INFINITY;
+    const float x[2] = {max_nan(v, kFloor), kFloor};
+    st.fold<2>(x, v, c2, tid < extras, [&](int j) { return j == 0 ? v : -INFINITY; });
   }
   for (int b = 0; b < nvec; b += kRowUnroll * kRowThreads) {
-    uint4 v[kRowUnroll] = {};
-    float x[kRowUnroll * E];
+    uint4 v[kRowUnroll];
 #pragma unroll
     for (int q = 0; q < kRowUnroll; ++q) {
       const int i = b + q * kRowThreads + tid;
-      if (i < nvec) v[q] = __ldg(vecs + i);
+      v[q] = i < nvec ? __ldg(vecs + i) : make_uint4(Type::neg_inf, Type::neg_inf, Type::neg_inf, Type::neg_inf);
     }
+    float x[kRowUnroll * E], cmax = -INFINITY;
 #pragma unroll
     for (int q = 0; q < kRowUnroll; ++q) {
-      const int i = b + q * kRowThreads + tid;
+      cmax = fmaxf(cmax, Type::top(v[q]));
       float w[E];
-      widen(v[q], w, T());
+      Type::floored(v[q], w);
 #pragma unroll
-      for (int j = 0; j < E; ++j) x[q * E + j] = i < nvec ? w[j] : -INFINITY;
+      for (int j = 0; j < E; ++j) x[q * E + j] = w[j];
     }
-    st.fold<kRowUnroll * E>(x, c2, b + tid < nvec);
+    st.fold<kRowUnroll * E>(x, cmax, c2, b + tid < nvec, [&](int j) {
+      const int i = b + (j / E) * kRowThreads + tid;
+      return i < nvec ? row_value(base[first_id + i * E + j % E]) : -INFINITY;
+    });
   }
 
   // ---- merge lanes, then warps
   {
-    float s = st.s, u = st.u, n = st.own;
+    const float f = fmaf(-st.delta, kLn2, 1.f);                     // back from ref to c2 m: 2^-delta
+    float s = st.s * f, u = fmaf(-st.delta, st.s, st.u) * f, n = st.own;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -215,165 +332,201 @@ logits_rows_kernel(const RowsArgs args) {
   if (tid == 0) { n_owner = 0; n_cand = 0; }
   __syncthreads();
   if (tid == 0) {
-    float M = -INFINITY;
-    for (int w = 0; w < kRowThreads / 32; ++w) M = fmaxf(M, sh_m[w]);
-    float r = 0.f, uu = 0.f;
-    int at_max = 0;
-    for (int w = 0; w < kRowThreads / 32; ++w) {
-      if (sh_m[w] == M) {
-        r += sh_s[w];
-        uu += sh_u[w];
-        at_max += sh_n[w];
-      } else {
-        const float tot = sh_s[w] + (float)sh_n[w];
-        if (sh_m[w] > -INFINITY) {
-          const float d = fmaxf((sh_m[w] - M) * c2, -1000.f), sc = fast_ex2(d);
-          r = fmaf(tot, sc, r);
-          uu = fmaf(sc, fmaf(d, tot, sh_u[w]), uu);
-        } else {
-          r += sh_s[w];                                             // nothing, or the NaN that a NaN entry left
+    RowSlice& o = sh_mine;
+    o.m = -INFINITY;
+    for (int w = 0; w < kWarps; ++w) o.m = fmaxf(o.m, sh_m[w]);
+    o.r = o.u = 0.f;
+    o.owners = 0;
+    for (int w = 0; w < kWarps; ++w) add_slice(sh_m[w], sh_s[w], sh_u[w], sh_n[w], c2, o.m, o.r, o.u, o.owners);
+    if (o.owners > 1) { o.r += (float)(o.owners - 1); o.owners = 1; }
+  }
+
+  // ---- the slice's k largest, falling, into sh_mine.top
+  if (k > 0) {
+    const bool holds = tid < nvec || tid < extras;
+    const uint32_t mine = holds ? (order_key(st.lane_max) >> kShift) : 0u;
+    uint32_t tau = 0u;                                              // largest class with at least k lane maxima in or above it
+#pragma unroll 1
+    for (int bit = 31 - kShift; bit >= 0; --bit) {
+      const uint32_t c = tau | (1u << bit);
+      if (__syncthreads_count(mine >= c) >= k) tau = c;
+    }
+    tau = max(tau, 1u);                                             // 0 is NaN's class
+    if (mine >= tau) owners[atomicAdd(&n_owner, 1)] = tid;
+    if (tid < kMaxTop) sh_mine.top[tid] = 0ull;
+    __syncthreads();
+    const int per_lane = (nvec + kRowThreads - 1) / kRowThreads;
+    auto offer = [&](float x, int id, uint32_t least) {
+      const uint32_t key = order_key(x);
+      if ((key >> kShift) >= least) {
+        const int at = atomicAdd(&n_cand, 1);
+        if (at < kRowCandidates) cand[at] = pack_entry(key, id);
+      }
+    };
+    // entries of class `least` or above, from the lanes whose maximum is
+    auto collect = [&](uint32_t least) {
+      if (tid < extras && mine >= least) offer(row_value(base[extra_id(tid)]), extra_id(tid), least);
+      const int items = n_owner * per_lane;
+      for (int w = tid; w < items; w += kRowThreads) {
+        const int i = (w % per_lane) * kRowThreads + owners[w / per_lane];
+        if (i >= nvec) continue;
+        float x[E];
+        Type::entries(__ldg(vecs + i), x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) offer(x[j], first_id + i * E + j, least);
+      }
+      __syncthreads();
+    };
+    bool done = false;
+    // many lanes tie at tau, or tau is the masked entries' -inf: only what is above it is collected that way
+    const bool many = n_owner > 4 * k + 32 || tau <= (kKeyNegInf >> kShift);
+    if (!many) {
+      collect(tau);
+      done = n_cand >= k && n_cand <= kRowCandidates;
+    }
+    if (!done) {
+      __syncthreads();
+      if (tid == 0) { n_cand = 0; n_owner = 0; }
+      __syncthreads();
+      if (mine > tau) owners[atomicAdd(&n_owner, 1)] = tid;
+      __syncthreads();
+      collect(tau + 1u);
+      if (n_cand <= kRowCandidates - k) {
+        // then entries of tau's class in the order of their ids until there are k.  A class is one value: what a
+        // 16-bit type's key drops is constant
+        int have = n_cand;
+        for (int b = 0; b < n_local && have < k; b += kRowThreads) {
+          const int id = b + tid < n_local ? local_id(b + tid) : -1;
+          uint32_t key = 0u;
+          if (id >= 0) key = order_key(row_value(base[id]));
+          const bool hit = id >= 0 && (key >> kShift) == tau;
+          const uint32_t votes = __ballot_sync(0xffffffffu, hit);
+          if (lane == 0) sh_scan[warp] = __popc(votes);
+          __syncthreads();
+          int before = 0, total = 0;
+          for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += sh_scan[w];
+            total += sh_scan[w];
+          }
+          const int at = have + before + __popc(votes & ((1u << lane) - 1u));
+          if (hit && at < k) cand[at] = pack_entry(key, id);
+          have = min(k, have + total);
+          __syncthreads();
         }
+        if (tid == 0) n_cand = max(have, n_cand);
+        done = true;
+        __syncthreads();
       }
     }
-    if (at_max > 1) r += (float)(at_max - 1);
+    if (done) {
+      const int n = n_cand;
+      for (int c = tid; c < n; c += kRowThreads) {
+        const unsigned long long e = cand[c];
+        int rank = 0;
+        for (int o = 0; o < n; ++o) rank += cand[o] > e ? 1 : 0;
+        if (rank < k) sh_mine.top[rank] = e;
+      }
+    } else {
+      // a few lanes hold hundreds of entries above the bound: k passes, each for the best entry below the last one
+      unsigned long long last = ~0ull;
+      for (int at = 0; at < k && last != 0ull; ++at) {
+        unsigned long long best = 0ull;
+        for (int i = tid; i < n_local; i += kRowThreads) {
+          const int id = local_id(i);
+          const uint32_t key = order_key(row_value(base[id]));
+          const unsigned long long e = key ? pack_entry(key, id) : 0ull;
+          if (e < last && e > best) best = e;
+        }
+        __syncthreads();
+        cand[tid] = best;
+        __syncthreads();
+        for (int o = kRowThreads / 2; o > 0; o >>= 1) {
+          if (tid < o && cand[tid + o] > cand[tid]) cand[tid] = cand[tid + o];
+          __syncthreads();
+        }
+        last = cand[0];
+        if (tid == 0) sh_mine.top[at] = last;
+      }
+    }
+  }
+  __syncthreads();
+
+  // ---- the slices of the row together
+  if (n_slice > 1) {
+    cluster.sync();
+    for (int i = tid; i < n_slice * k; i += kRowThreads) cand[i] = cluster.map_shared_rank(&sh_mine, i / k)->top[i % k];
+    if (tid < n_slice) {
+      const RowSlice* o = cluster.map_shared_rank(&sh_mine, tid);
+      all_m[tid] = o->m; all_r[tid] = o->r; all_u[tid] = o->u; all_n[tid] = o->owners;
+    }
+    if (tid < kMaxTop) sh_rank[tid] = 0;
+    cluster.barrier_arrive();                                       // done with the other blocks' memory
+    __syncthreads();
+  }
+  if (tid == 0) {
+    float M = sh_mine.m, r = sh_mine.r, uu = sh_mine.u;
+    int n = sh_mine.owners;
+    if (n_slice > 1) {
+      M = -INFINITY;
+      for (int j = 0; j < n_slice; ++j) M = fmaxf(M, all_m[j]);
+      r = uu = 0.f;
+      n = 0;
+      for (int j = 0; j < n_slice; ++j) add_slice(all_m[j], all_r[j], all_u[j], all_n[j], c2, M, r, uu, n);
+    }
+    if (n > 1) r += (float)(n - 1);
     const bool nothing = M == -INFINITY && r == 0.f;                // no entry has a probability
     const float ln_s = nothing ? 0.f : (M == -INFINITY ? __uint_as_float(0x7FC00000u) : log1pf(r));
     sh_row[0] = M;
     sh_row[1] = ln_s;
-    if (args.partials) args.partials[row] = make_float4(M, r, 0.f, 0.f);
-    if (args.lse) args.lse[row] = nothing ? -INFINITY : fmaf(args.kappa, M, ln_s);
-    if (args.norm) args.norm[row] = make_float2(M, ln_s);
-    if (args.entropy) args.entropy[row] = nothing ? 0.f : max_nan(ln_s - kLn2 * uu / (1.f + r), 0.f);
-    if (args.logp) {
-      int y = args.targets[row];
-      const bool bad = y < 0 || y >= V;
-      if (bad && args.status) {                                     // the LM-head calls report and clamp
-        atomicOr(args.status, kStatusBadTarget);
-        y = y < 0 ? 0 : V - 1;
-      }
-      args.logp[row] = bad && !args.status ? __uint_as_float(0x7FC00000u)
-                       : nothing           ? -INFINITY
-                                           : args.kappa * (row_value(base[y]) - M) - ln_s;
-    }
-  }
-  if (k == 0) return;
-
-  // ---- the k largest
-  const bool holds = tid < nvec || tid < extras;
-  const uint32_t mine = holds ? (order_key(st.lane_max) >> kShift) : 0u;
-  uint32_t tau = 0u;                                                // largest class with at least k lane maxima in or above it
-#pragma unroll 1
-  for (int bit = 31 - kShift; bit >= 0; --bit) {
-    const uint32_t c = tau | (1u << bit);
-    if (__syncthreads_count(mine >= c) >= k) tau = c;
-  }
-  tau = max(tau, 1u);                                               // 0 is NaN's class
-  if (mine >= tau) owners[atomicAdd(&n_owner, 1)] = tid;
-  __syncthreads();
-  const int per_lane = (nvec + kRowThreads - 1) / kRowThreads;
-  auto offer = [&](float x, int id, uint32_t least) {
-    const uint32_t key = order_key(x);
-    if ((key >> kShift) >= least) {
-      const int at = atomicAdd(&n_cand, 1);
-      if (at < kRowCandidates) cand[at] = pack_entry(key, id);
-    }
-  };
-  // entries of class `least` or above, from the lanes whose maximum is
-  auto collect = [&](uint32_t least) {
-    if (tid < extras && mine >= least) offer(row_value(base[extra_id(tid)]), extra_id(tid), least);
-    const int items = n_owner * per_lane;
-    for (int w = tid; w < items; w += kRowThreads) {
-      const int i = (w % per_lane) * kRowThreads + owners[w / per_lane];
-      if (i >= nvec) continue;
-      float x[E];
-      widen(__ldg(vecs + i), x, T());
-#pragma unroll
-      for (int j = 0; j < E; ++j) offer(x[j], head + i * E + j, least);
-    }
-    __syncthreads();
-  };
-  bool done = false;
-  // many lanes tie at tau, or tau is the masked entries' -inf: only what is above it is collected that way
-  const bool many = n_owner > 4 * k + 32 || tau <= (kKeyNegInf >> kShift);
-  if (!many) {
-    collect(tau);
-    done = n_cand >= k && n_cand <= kRowCandidates;
-  }
-  if (!done) {
-    __syncthreads();
-    if (tid == 0) { n_cand = 0; n_owner = 0; }
-    __syncthreads();
-    if (mine > tau) owners[atomicAdd(&n_owner, 1)] = tid;
-    __syncthreads();
-    collect(tau + 1u);
-    if (n_cand <= kRowCandidates - k) {
-      // then entries of tau's class in the order of their ids until there are k.  A class is one value: what a
-      // 16-bit type's key drops is constant
-      int have = n_cand;
-      for (int b = 0; b < V && have < k; b += kRowThreads) {
-        const int id = b + tid;
-        uint32_t key = 0u;
-        if (id < V) key = order_key(row_value(base[id]));
-        const bool hit = id < V && (key >> kShift) == tau;
-        const uint32_t votes = __ballot_sync(0xffffffffu, hit);
-        if (lane == 0) sh_scan[warp] = __popc(votes);
-        __syncthreads();
-        int before = 0, total = 0;
-        for (int w = 0; w < kRowThreads / 32; ++w) {
-          if (w < warp) before += sh_scan[w];
-          total += sh_scan[w];
+    if (slice == 0) {
+      if (args.partials) args.partials[row] = make_float4(M, r, 0.f, 0.f);
+      if (args.lse) args.lse[row] = nothing ? -INFINITY : fmaf(args.kappa, M, ln_s);
+      if (args.norm) args.norm[row] = make_float2(M, ln_s);
+      if (args.entropy) args.entropy[row] = nothing ? 0.f : max_nan(ln_s - kLn2 * uu / (1.f + r), 0.f);
+      if (args.logp) {
+        int y = args.targets[row];
+        const bool bad = y < 0 || y >= V;
+        if (bad && args.status) {                                   // the LM-head calls report and clamp
+          atomicOr(args.status, kStatusBadTarget);
+          y = y < 0 ? 0 : V - 1;
         }
-        const int at = have + before + __popc(votes & ((1u << lane) - 1u));
-        if (hit && at < k) cand[at] = pack_entry(key, id);
-        have = min(k, have + total);
-        __syncthreads();
+        args.logp[row] = bad && !args.status ? __uint_as_float(0x7FC00000u)
+                         : nothing           ? -INFINITY
+                                             : args.kappa * (row_value(base[y]) - M) - ln_s;
       }
-      if (tid == 0) n_cand = max(have, n_cand);
-      done = true;
-      __syncthreads();
     }
   }
-  const float M = sh_row[0], ln_s = sh_row[1];
-  auto put = [&](int at, unsigned long long entry) {
-    const float x = key_value((uint32_t)(entry >> 32));
-    args.top_ids[(size_t)row * k + at] = entry == 0ull ? -1 : (int)~(uint32_t)entry;
-    args.top_logp[(size_t)row * k + at] = M == -INFINITY && ln_s == 0.f ? (entry == 0ull ? x : -INFINITY)
-                                                                        : args.kappa * (x - M) - ln_s;
-  };
-  if (done) {
-    const int n = n_cand;
-    for (int c = tid; c < max(n, k); c += kRowThreads) {
-      if (c >= n) { put(c, 0ull); continue; }                       // fewer than k entries are numbers
-      const unsigned long long e = cand[c];
-      int rank = 0;
-      for (int o = 0; o < n; ++o) rank += cand[o] > e ? 1 : 0;
-      if (rank < k) put(rank, e);
-    }
-    return;
-  }
-  // a few lanes hold hundreds of entries above the bound: k passes, each for the best entry below the last one
-  unsigned long long last = ~0ull;
-  for (int at = 0; at < k; ++at) {
-    unsigned long long best = 0ull;
-    for (int id = tid; id < V; id += kRowThreads) {
-      const uint32_t key = order_key(row_value(base[id]));
-      const unsigned long long e = key ? pack_entry(key, id) : 0ull;
-      if (e < last && e > best) best = e;
-    }
+  if (k > 0) {
     __syncthreads();
-    cand[tid] = best;
-    __syncthreads();
-    for (int o = kRowThreads / 2; o > 0; o >>= 1) {
-      if (tid < o && cand[tid + o] > cand[tid]) cand[tid] = cand[tid + o];
-      __syncthreads();
-    }
-    last = cand[0];
-    if (tid == 0) put(at, last);
-    if (last == 0ull) {
-      for (int c = at + 1 + tid; c < k; c += kRowThreads) put(c, 0ull);
-      return;
+    const float M = sh_row[0], ln_s = sh_row[1];
+    auto put = [&](int at, unsigned long long entry) {
+      const float x = key_value((uint32_t)(entry >> 32));
+      args.top_ids[(size_t)row * k + at] = entry == 0ull ? -1 : (int)~(uint32_t)entry;
+      args.top_logp[(size_t)row * k + at] = M == -INFINITY && ln_s == 0.f ? (entry == 0ull ? x : -INFINITY)
+                                                                          : args.kappa * (x - M) - ln_s;
+    };
+    if (n_slice == 1) {
+      if (tid < k) put(tid, sh_mine.top[tid]);                      // 0: fewer than k entries are numbers
+    } else {
+      // an entry's place: how many of every slice's list are better
+      for (int w = tid; w < k * n_slice; w += kRowThreads) {
+        const unsigned long long e = sh_mine.top[w % k];
+        const unsigned long long* list = cand + (w / k) * k;
+        int lo = 0, hi = k;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (list[mid] > e) lo = mid + 1; else hi = mid;
+        }
+        if (e != 0ull && lo > 0) atomicAdd(&sh_rank[w % k], lo);
+      }
+      int used = 0;
+      for (int i = tid; i < n_slice * k; i += kRowThreads) used += cand[i] != 0ull ? 1 : 0;
+      used = __syncthreads_count(used > 0) + __syncthreads_count(used > 1);      // at most two a thread
+      if (tid < k && sh_mine.top[tid] != 0ull && sh_rank[tid] < k) put(sh_rank[tid], sh_mine.top[tid]);
+      if (slice == 0 && tid >= used && tid < k) put(tid, 0ull);
     }
   }
+  if (n_slice > 1) cluster.barrier_wait();                          // no block leaves while another reads its list
 }
 
 // ------------------------------------------------------------------------------------------

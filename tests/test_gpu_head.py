@@ -59,7 +59,7 @@ def check_scores(out, hidden, W, targets, k, kappa, exact_ids):
 
 
 # sizes: one token, tile edges of 128 / 256 rows and 256 columns, a vocabulary of one entry, of less than a chunk
-SIZES = [(1, 64, 1000, 5), (3, 8, 1, 1), (2, 8, 7, 7), (5, 72, 31, 8), (127, 64, 255, 9), (129, 136, 257, 32),
+SIZES = [(1, 64, 1000, 5), (16, 72, 20001, 3), (17, 128, 2500, 20), (33, 64, 40003, 32), (64, 200, 3000, 8), (65, 200, 3000, 8), (3, 8, 1, 1), (2, 8, 7, 7), (5, 72, 31, 8), (127, 64, 255, 9), (129, 136, 257, 32),
          (300, 256, 4099, 20), (257, 512, 2048, 0), (700, 64, 20000, 32)]
 
 
@@ -248,7 +248,7 @@ def check_distill(p, hidden, W, ids, teacher, weights, tensor_path, grad_loss=No
     return out, d_h, d_W, ws
 
 
-DISTILL_SIZES = [(1, 64, 1000, 5), (3, 8, 5, 5), (9, 16, 40, 1), (129, 136, 257, 32), (300, 256, 4099, 20), (70, 64, 700, 128)]
+DISTILL_SIZES = [(1, 64, 1000, 5), (20, 64, 3001, 7), (40, 136, 2000, 33), (64, 64, 500, 4), (16, 72, 20001, 3), (17, 128, 2500, 20), (33, 64, 40003, 32), (64, 200, 3000, 8), (65, 200, 3000, 8), (3, 8, 5, 5), (9, 16, 40, 1), (129, 136, 257, 32), (300, 256, 4099, 20), (70, 64, 700, 128)]
 
 
 @pytest.mark.parametrize("T,H,V,K", DISTILL_SIZES)

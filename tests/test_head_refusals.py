@@ -44,7 +44,7 @@ def test_workspace_sizes(lib):
     big = dict(T=8192, H=2048, V=151936)
     fwd = U.head_workspace_bytes(params(**big, top_k=32), backward=False)
     bwd = U.head_workspace_bytes(params(**big, top_k=32, dw_dtype="bf16"))
-    assert fwd < 64 << 20
+    assert fwd < 128 << 20
     assert 8192 * 151936 * 2 <= bwd <= 8192 * 151936 * 2 + (64 << 20)
     more = U.head_workspace_bytes(params(**big, top_k=32, dw_dtype="bf16", dw_accumulate=True))
     assert more - bwd >= 151936 * 2048 * 4
