@@ -2,6 +2,7 @@
 #pragma once
 
 #include "scores.cuh"
+#include "sgemm.cuh"
 #include "small_batch.cuh"
 
 namespace ulorl {
@@ -45,6 +46,14 @@ static int validate_head(const ulorl_head_params_t* p) {
   if (p->top_k > ULORL_MAX_LIST) return ULORL_ERR_UNSUPPORTED;
   if (p->H % 8 != 0) return ULORL_ERR_UNSUPPORTED;
   return ULORL_OK;
+}
+
+// Parts over k of an M x N float32 contraction: as many as there are multiprocessors for, 256 values of k or more each.
+static int sgemm_parts(const HeadPlan& pl, int M, int N, int K, int* k_part) {
+  const long tiles = (long)((M + kSgTile - 1) / kSgTile) * ((N + kSgTile - 1) / kSgTile);
+  long parts = std::max(1L, std::min(pl.sms / std::max(1L, tiles), (long)K / 256));
+  *k_part = (int)align_up((size_t)((K + parts - 1) / parts), kSgK);
+  return (K + *k_part - 1) / *k_part;
 }
 
 static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
@@ -131,6 +140,11 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   pl.off_panel = off;
   off = align_up(off + (size_t)panel * pl.dz_ld * (pl.tensor ? 2 : 4), 1024);
   if (pl.dw_acc) { pl.off_dw_acc = off; off = align_up(off + sizeof(float) * (size_t)V * (size_t)H, 1024); }
+  if (!pl.tensor && p->dtype == ULORL_F32) {      // float32 contractions cut over k
+    pl.off_parts = off;
+    // tiles x parts is at most the multiprocessor count, so are the parts' rows, in tiles, of any contraction here
+    off = align_up(off + sizeof(float) * (size_t)pl.sms * kSgTile * (size_t)H, 1024);
+  }
   if (pl.dh_parts > 1) {
     pl.off_parts = off;
     off = align_up(off + sizeof(float) * (size_t)pl.dh_parts * (size_t)pl.dh_part_rows * (size_t)H, 1024);
@@ -170,14 +184,41 @@ static int run_sweep(const ulorl_head_params_t* p, const HeadPlan& pl, int mode,
   }
 }
 
-// panel[i, v] = hidden[t0 + i] . W[v] in float32 on CUDA cores.
-template <typename TIn>
-static int simt_logits_panel(const ulorl_head_params_t* p, const void* hidden, const void* W, int t0, int rows, float* panel,
-                             size_t ld, cudaStream_t stream) {
+template <bool kAAlongK, bool kBAlongK>
+static int run_sgemm(const HeadPlan& pl, const float* A, size_t lda, const float* B, size_t ldb, float* C, size_t ldc, int M, int N,
+                     int K, int accumulate, float* scratch, cudaStream_t stream) {
+  SgemmArgs a{};
+  a.A = A; a.B = B; a.lda = lda; a.ldb = ldb;
+  a.M = M; a.N = N; a.K = K;
+  int parts = 1;
+  a.k_part = (int)align_up((size_t)K, kSgK);
+  if (scratch) parts = sgemm_parts(pl, M, N, K, &a.k_part);
+  a.C = parts > 1 ? scratch : C;
+  a.ldc = parts > 1 ? (size_t)N : ldc;
+  a.part_stride = parts > 1 ? (size_t)M * (size_t)N : 0;
+  a.accumulate = parts > 1 ? 0 : accumulate;
+  const dim3 grid((N + kSgTile - 1) / kSgTile, (M + kSgTile - 1) / kSgTile, parts);
+  sgemm_kernel<kAAlongK, kBAlongK><<<grid, kSgThreads, 0, stream>>>(a);
+  ULORL_LAUNCH_CHECK();
+  if (parts > 1) {                                                  // rows of the result are contiguous here: ldc = N
+    const size_t n = (size_t)M * (size_t)N;
+    sgemm_parts_kernel<<<(unsigned)((n / 4 + 255) / 256), 256, 0, stream>>>(scratch, parts, n, n, C, accumulate);
+    ULORL_LAUNCH_CHECK();
+  }
+  return ULORL_OK;
+}
+
+// panel[i, v] = hidden[t0 + i] . W[v] in float32 on CUDA cores (bf16 operands: the cross-check of the tensor path).
+static int simt_logits_panel(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, int t0, int rows,
+                             float* panel, size_t ld, cudaStream_t stream) {
+  const size_t H = (size_t)p->H;
+  if (p->dtype == ULORL_F32)
+    return run_sgemm<true, true>(pl, static_cast<const float*>(hidden) + (size_t)t0 * H, H, static_cast<const float*>(W), H, panel, ld,
+                                 rows, p->V, p->H, 0, nullptr, stream);
   const dim3 grid((p->V + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
-  simt_gemm_kernel<TIn, TIn, float><<<grid, kSimtThreads, 0, stream>>>(
-      static_cast<const TIn*>(hidden) + (size_t)t0 * p->H, (size_t)p->H, 1, static_cast<const TIn*>(W), 1, (size_t)p->H,
-      panel, ld, rows, p->V, p->H, 0);
+  simt_gemm_kernel<__nv_bfloat16, __nv_bfloat16, float><<<grid, kSimtThreads, 0, stream>>>(
+      static_cast<const __nv_bfloat16*>(hidden) + (size_t)t0 * H, H, 1, static_cast<const __nv_bfloat16*>(W), 1, H, panel, ld, rows,
+      p->V, p->H, 0);
   return check_launch();
 }
 
@@ -219,9 +260,7 @@ static int launch_small(const ulorl_head_params_t* p, const HeadPlan& pl, const 
 // logits[i, v] = hidden[t0 + i] . W[v] in float32 for the paths that go through a panel of logits.
 static int logits_panel(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, int t0, int rows,
                         float* logits, uint8_t* ws, cudaStream_t stream) {
-  if (!pl.small)
-    return p->dtype == ULORL_F32 ? simt_logits_panel<float>(p, hidden, W, t0, rows, logits, pl.logits_ld, stream)
-                                 : simt_logits_panel<__nv_bfloat16>(p, hidden, W, t0, rows, logits, pl.logits_ld, stream);
+  if (!pl.small) return simt_logits_panel(p, pl, hidden, W, t0, rows, logits, pl.logits_ld, stream);
   int* status = reinterpret_cast<int*>(ws + pl.off_status);
   if (p->T <= 16) return launch_small<16>(p, pl, hidden, W, logits, status, stream);
   if (p->T <= 32) return launch_small<32>(p, pl, hidden, W, logits, status, stream);
@@ -383,8 +422,7 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       const dim3 gdh((H + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
       const dim3 gdw((H + kSimtTile - 1) / kSimtTile, (V + kSimtTile - 1) / kSimtTile);
       const bool f32 = p->dtype == ULORL_F32;
-      st = f32 ? simt_logits_panel<float>(p, hidden, W, t0, rows, dz, ld, stream)
-               : simt_logits_panel<__nv_bfloat16>(p, hidden, W, t0, rows, dz, ld, stream);
+      st = simt_logits_panel(p, pl, hidden, W, t0, rows, dz, ld, stream);
       if (st != ULORL_OK) return st;
       dz_rows_f32_kernel<<<gdz, 256, 0, stream>>>(dz, ld, V, t0, p->inv_temperature, row_p, row_ins, targets);
       ULORL_LAUNCH_CHECK();
@@ -393,13 +431,13 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
         if (st != ULORL_OK) return st;
       }
       if (f32) {
-        simt_gemm_kernel<float, float, float><<<gdh, kSimtThreads, 0, stream>>>(
-            dz, ld, 1, static_cast<const float*>(W), (size_t)H, 1, static_cast<float*>(d_hidden) + (size_t)t0 * H, (size_t)H,
-            rows, H, V, 0);
-        ULORL_LAUNCH_CHECK();
-        simt_gemm_kernel<float, float, float><<<gdw, kSimtThreads, 0, stream>>>(
-            dz, 1, ld, static_cast<const float*>(hidden) + (size_t)t0 * H, (size_t)H, 1, d_W, (size_t)H, V, H, rows, acc);
-        ULORL_LAUNCH_CHECK();
+        float* scratch = reinterpret_cast<float*>(ws + pl.off_parts);
+        st = run_sgemm<true, false>(pl, dz, ld, static_cast<const float*>(W), (size_t)H, static_cast<float*>(d_hidden) + (size_t)t0 * H,
+                                    (size_t)H, rows, H, V, 0, scratch, stream);
+        if (st != ULORL_OK) return st;
+        st = run_sgemm<false, false>(pl, dz, ld, static_cast<const float*>(hidden) + (size_t)t0 * H, (size_t)H, d_W, (size_t)H, V, H,
+                                     rows, acc, scratch, stream);
+        if (st != ULORL_OK) return st;
       } else {
         simt_gemm_kernel<float, __nv_bfloat16, __nv_bfloat16><<<gdh, kSimtThreads, 0, stream>>>(
             dz, ld, 1, static_cast<const __nv_bfloat16*>(W), (size_t)H, 1,

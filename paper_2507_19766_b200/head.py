@@ -78,7 +78,7 @@ def _raise(code: int, what: str):
     raise UlorlError(f"{what} failed: {status_string(code)} ({code})")
 
 
-def _take(t: Optional[torch.Tensor], name: str, dtype, n: int, device, optional: bool = False):
+def _take(t: Optional[torch.Tensor], name: str, dtype, n: int, device: int, optional: bool = False):
     """The tensor's device pointer, after the checks that keep the kernels inside it."""
     if t is None:
         if optional:
@@ -86,23 +86,26 @@ def _take(t: Optional[torch.Tensor], name: str, dtype, n: int, device, optional:
         raise UlorlError(f"{name} is missing")
     if t.dtype != dtype or t.numel() != n:
         raise UlorlError(f"{name}: expected {n} elements of {dtype}, got {t.numel()} of {t.dtype}")
-    if t.device != device or not t.is_contiguous():
-        raise UlorlError(f"{name}: expected a contiguous tensor on {device}")
+    if not t.is_cuda or t.get_device() != device or not t.is_contiguous():
+        raise UlorlError(f"{name}: expected a contiguous tensor on cuda:{device}")
     return t.data_ptr()
 
 
-def _device_of(t: torch.Tensor, name: str):
+def _device_of(t: torch.Tensor, name: str) -> int:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise UlorlError(f"{name}: expected a CUDA tensor (there is no CPU path)")
-    return t.device
+    return t.get_device()
 
 
-def _on(device):
+_SAME = contextlib.nullcontext()
+
+
+def _on(device: int):
     """Makes the tensors' device the current one for the call, if it is not."""
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return _SAME if device == torch.cuda.current_device() else torch.cuda.device(device)
 
 
-def _stream(device) -> int:
+def _stream(device: int) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
 
@@ -115,15 +118,16 @@ def head_workspace_bytes(p: HeadParams, backward: bool = True) -> int:
 
 def alloc_head_workspace(p: HeadParams, device, backward: bool = True) -> torch.Tensor:
     """Scratch of the calls with these params; backward=False is enough (and far smaller) for the forward ones."""
-    with _on(torch.device(device)) if torch.device(device).index is not None else contextlib.nullcontext():
+    device = torch.device(device)
+    with _SAME if device.index is None else _on(device.index):      # sizes go by the device's multiprocessor count
         return torch.empty(head_workspace_bytes(p, backward), dtype=torch.uint8, device=device)
 
 
-def _workspace(p: HeadParams, workspace, device, backward: bool):
+def _workspace(p: HeadParams, workspace, device: int, backward: bool):
     if workspace is None:
-        workspace = alloc_head_workspace(p, device, backward)
-    if workspace.device != device or not workspace.is_contiguous():
-        raise UlorlError(f"workspace: expected a contiguous tensor on {device}")
+        workspace = alloc_head_workspace(p, torch.device("cuda", device), backward)
+    if not workspace.is_cuda or workspace.get_device() != device or not workspace.is_contiguous():
+        raise UlorlError(f"workspace: expected a contiguous tensor on cuda:{device}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -143,11 +147,11 @@ def token_scores(p: HeadParams, hidden, W, targets=None, out: Optional[ScoresOut
     f32, T, k = torch.float32, p.T, p.top_k
     with _on(device):
         if out is None:
-            rows = torch.empty(5, T, dtype=f32, device=device)
+            rows = torch.empty(5, T, dtype=f32, device=hidden.device)
             # norm first: pairs need eight-byte alignment
             out = ScoresOut(rows[2] if targets is not None else None, rows[3], rows[4], rows[:2].view(T, 2),
-                            torch.empty(T, k, dtype=torch.int32, device=device) if k else None,
-                            torch.empty(T, k, dtype=f32, device=device) if k else None)
+                            torch.empty(T, k, dtype=torch.int32, device=hidden.device) if k else None,
+                            torch.empty(T, k, dtype=f32, device=hidden.device) if k else None)
         workspace, pws, nws = _workspace(p, workspace, device, False)
         code = lib.ulorl_token_scores(
             ctypes.byref(cp), ph, pw, pt, _take(out.logp, "logp", f32, T, device, targets is None),
@@ -163,7 +167,7 @@ def _grad_outputs(p: HeadParams, d_hidden, d_W, hidden, device):
     if d_hidden is None:
         d_hidden = torch.empty_like(hidden)
     if d_W is None:
-        d_W = (torch.zeros if p.dw_accumulate else torch.empty)(p.V, p.H, dtype=_DTYPES[p.dw_dtype], device=device)
+        d_W = (torch.zeros if p.dw_accumulate else torch.empty)(p.V, p.H, dtype=_DTYPES[p.dw_dtype], device=hidden.device)
     return (d_hidden, d_W, _take(d_hidden, "d_hidden", _DTYPES[p.dtype], p.T * p.H, device),
             _take(d_W, "d_W", _DTYPES[p.dw_dtype], p.V * p.H, device))
 
@@ -203,18 +207,28 @@ def logits_scores(logits: torch.Tensor, targets=None, top_k: int = 0, inv_temper
     if (V > 1 and logits.stride(1) != 1) or ld < V:
         raise UlorlError("logits: a row must be contiguous and rows must not overlap")
     pt = _take(targets, "targets", torch.int32, T, device, optional=True)
-    f32, k = torch.float32, top_k
+    k = top_k
     with _on(device):
         if out is None:
-            rows = torch.empty(3, T, dtype=f32, device=device)
-            out = ScoresOut(rows[0] if targets is not None else None, rows[1], rows[2], None,
-                            torch.empty(T, k, dtype=torch.int32, device=device) if k > 0 else None,
-                            torch.empty(T, k, dtype=f32, device=device) if k > 0 else None)
-        code = lib.ulorl_logits_scores(
-            logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
-            _take(out.logp, "logp", f32, T, device, targets is None), _take(out.entropy, "entropy", f32, T, device, True),
-            _take(out.lse, "lse", f32, T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k <= 0),
-            _take(out.top_logp, "top_logp", f32, T * k, device, k <= 0), _stream(device))
+            # one allocation for all outputs: a decoding step's call is mostly what the host does
+            flat = torch.empty(T * (3 + 2 * max(k, 0)), dtype=torch.float32, device=logits.device)
+            at = flat.data_ptr()
+            ptrs = (at if pt is not None else None, at + 4 * T, at + 8 * T) + ((at + 12 * T, at + 4 * T * (3 + k)) if k > 0 else (None, None))
+            code = lib.ulorl_logits_scores(logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt, *ptrs, _stream(device))
+            if k > 0:
+                logp, entropy, lse, ids, top_logp = flat.split((T, T, T, T * k, T * k))
+                out = ScoresOut(logp if pt is not None else None, entropy, lse, None, ids.view(torch.int32).view(T, k),
+                                top_logp.view(T, k))
+            else:
+                logp, entropy, lse = flat.split((T, T, T))
+                out = ScoresOut(logp if pt is not None else None, entropy, lse, None, None, None)
+        else:
+            f32 = torch.float32
+            code = lib.ulorl_logits_scores(
+                logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
+                _take(out.logp, "logp", f32, T, device, targets is None), _take(out.entropy, "entropy", f32, T, device, True),
+                _take(out.lse, "lse", f32, T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k <= 0),
+                _take(out.top_logp, "top_logp", f32, T * k, device, k <= 0), _stream(device))
     if code != OK:
         _raise(code, "ulorl_logits_scores")
     return out
@@ -232,9 +246,9 @@ def distill_fwd(p: HeadParams, hidden, W, teacher_ids, teacher_logp, weights=Non
     pwt = _take(weights, "weights", f32, T, device, optional=True)
     with _on(device):
         if out is None:
-            rows = torch.empty(5, T, dtype=f32, device=device)
-            out = DistillOut(torch.empty(1, dtype=f32, device=device), rows[2], rows[3], rows[:2].view(T, 2), rows[4],
-                             torch.empty(T, k, dtype=f32, device=device))
+            rows = torch.empty(5, T, dtype=f32, device=hidden.device)
+            out = DistillOut(torch.empty(1, dtype=f32, device=hidden.device), rows[2], rows[3], rows[:2].view(T, 2), rows[4],
+                             torch.empty(T, k, dtype=f32, device=hidden.device))
         workspace, pws, nws = _workspace(p, workspace, device, False)
         code = lib.ulorl_distill_fwd(
             ctypes.byref(cp), ph, pw, pi, pl, pwt, _take(out.loss, "loss", f32, 1, device), _take(out.kl, "kl", f32, T, device),
