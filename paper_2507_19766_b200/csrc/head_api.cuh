@@ -277,7 +277,8 @@ static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   {
     std::lock_guard<std::mutex> lock(g_setup_mutex);
     if (!opted_in[dev]) {
-      if (cudaFuncSetAttribute(logits_rows_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+      if (cudaFuncSetAttribute(logits_rows_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+          cudaFuncSetAttribute(logits_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem) != cudaSuccess)
         return ULORL_ERR_CUDA;
       opted_in[dev] = true;
     }
@@ -288,6 +289,7 @@ static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)a.T * (unsigned)cluster, 1, 1);
   cfg.blockDim = dim3(kRowThreads, 1, 1);
+  cfg.dynamicSmemBytes = kRowSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;

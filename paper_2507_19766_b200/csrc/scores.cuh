@@ -136,7 +136,10 @@ struct RowsArgs {
 };
 
 constexpr int kRowThreads = 256;
-constexpr int kRowUnroll = 4;          // 16-byte loads a thread has in flight
+constexpr int kRowUnroll = 4;          // 16-byte vectors of a thread in a batch
+constexpr int kRowBatch = kRowUnroll * kRowThreads;       // vectors: 16 KB
+constexpr int kRowStages = 4;          // batches on their way or waiting in shared memory
+constexpr size_t kRowSmem = (size_t)kRowStages * kRowBatch * 16 + 128;
 constexpr int kRowCandidates = 512;
 constexpr int kRowMaxCluster = 16;
 
@@ -155,7 +158,7 @@ struct RowState {
   // folds in n entries: cmax is the largest of them, x their values, not below kFloor; `any`: the lane has some.  All lanes
   // of a warp together.  `exact` gives entry j as it is.
   template <int n, typename Exact>
-  __device__ __forceinline__ void fold(const float (&x)[n], float cmax, float c2, bool any, Exact exact) {
+  __device__ __forceinline__ void fold(float (&x)[n], float cmax, float c2, bool any, Exact exact) {
     if (any) lane_max = fmaxf(lane_max, cmax);
     const int ci = __float_as_int(cmax);
     const int wi = __reduce_max_sync(0xffffffffu, ci ^ ((ci >> 31) & 0x7FFFFFFF));    // ordered as integers
@@ -175,35 +178,31 @@ struct RowState {
     }
     float ls = 0.f, lu = 0.f;
     if (plain() || m == -INFINITY) {
-      constexpr int kChains = n >= 8 ? 4 : 1;
-      float2 a[kChains] = {}, b[kChains] = {};
-      const float2 cc = make_float2(c2, c2), nref = make_float2(-ref, -ref);
+      if (risen) {
+        // the maximum itself is left out before the sums (a peaked row's 1 - p is what the others add up to); of
+        // several equal ones the others count
+        float equal = 0.f;
 #pragma unroll
-      for (int j = 0; j < n; j += 2) {
-        const int q = (j / 2) % kChains;
-        const float2 t = fma2(make_float2(x[j], x[j + 1]), cc, nref);
-        const float2 e = make_float2(fast_ex2(t.x), fast_ex2(t.y));
-        a[q] = add2(a[q], e);
-        b[q] = fma2(e, t, b[q]);
-      }
-#pragma unroll
-      for (int q = 1; q < kChains; ++q) { a[0] = add2(a[0], a[q]); b[0] = add2(b[0], b[q]); }
-      ls = a[0].x + a[0].y;
-      lu = b[0].x + b[0].y;
-      if (risen && cmax == m) {
-        // the new maximum's own 1: taken off the sum where the others are a quarter of it or more, else they are added
-        // without it (a peaked row's 1 - p would lose its digits)
-        ls -= one();
-        lu -= delta;
-        own = 1.f;
-        if (ls < 0.25f) {
-          ls = -1.f;
-#pragma unroll
-          for (int j = 0; j < n; ++j) ls += x[j] == m ? 1.f : 0.f;
-#pragma unroll
-          for (int j = 0; j < n; ++j) ls += x[j] == m ? 0.f : fast_ex2(fmaf(x[j], c2, -ref));
+        for (int j = 0; j < n; ++j) {
+          const bool top = x[j] == m;
+          equal += top ? 1.f : 0.f;
+          x[j] = top ? kFloor : x[j];
+        }
+        if (equal > 0.f) {
+          own = 1.f;
+          ls = (equal - 1.f) * one();
         }
       }
+      constexpr int kChains = n >= 8 ? 4 : 1;
+      float a[kChains] = {}, b[kChains] = {};
+#pragma unroll
+      for (int j = 0; j < n; ++j) {
+        const float t = fmaf(x[j], c2, -ref), e = fast_ex2(t);
+        a[j % kChains] += e;
+        b[j % kChains] = fmaf(e, t, b[j % kChains]);
+      }
+#pragma unroll
+      for (int q = 0; q < kChains; ++q) { ls += a[q]; lu += b[q]; }
     } else {
       float ties = 0.f;
 #pragma unroll 1
@@ -251,7 +250,7 @@ __device__ __forceinline__ void add_slice(float m, float s, float u, int n, floa
 // 256 lane maxima bounds the k-th largest entry of the slice from below, and entries at or above it sit in lanes whose
 // maximum is: only their few vectors are read again.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 3)
 logits_rows_kernel(const RowsArgs args) {
   namespace cg = cooperative_groups;
   using Type = RowType<T>;
@@ -262,10 +261,14 @@ logits_rows_kernel(const RowsArgs args) {
   const int n_slice = (int)cluster.num_blocks(), slice = (int)cluster.block_rank();
   __shared__ float sh_m[kWarps], sh_s[kWarps], sh_u[kWarps];
   __shared__ int sh_n[kWarps];
+  extern __shared__ uint8_t ring_raw[];
+  __shared__ __align__(8) uint64_t bar_full[kRowStages], bar_empty[kRowStages];
+  __shared__ volatile int abort_flag;
   __shared__ RowSlice sh_mine;
   __shared__ float all_m[kRowMaxCluster], all_r[kRowMaxCluster], all_u[kRowMaxCluster];
   __shared__ int all_n[kRowMaxCluster];
   __shared__ float sh_row[2];                                       // m, ln s
+  __shared__ uint32_t sh_tau;
   __shared__ unsigned long long cand[kRowCandidates];
   __shared__ int owners[kRowThreads];
   __shared__ int n_owner, n_cand, sh_scan[kWarps + 1], sh_rank[kMaxTop];
@@ -289,19 +292,26 @@ logits_rows_kernel(const RowsArgs args) {
   };
   const float c2 = args.kappa * kLog2e;
 
+  const uint4* ring_ptr = reinterpret_cast<const uint4*>((reinterpret_cast<uintptr_t>(ring_raw) + 127u) & ~(uintptr_t)127u);
+  const uint32_t ring = ptx::smem_u32(ring_ptr);
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < kRowStages; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&bar_full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&bar_empty[i]), kWarps);
+    }
+    ptx::mbar_fence_init();
+    ptx::fence_async_proxy();
+  }
+  __syncthreads();
+
   RowState st;
   if (slice == 0) {
     const float v = tid < extras ? row_value(base[extra_id(tid)]) : -INFINITY;
-    const float x[2] = {max_nan(v, kFloor), kFloor};
+    float x[2] = {max_nan(v, kFloor), kFloor};
     st.fold<2>(x, v, c2, tid < extras, [&](int j) { return j == 0 ? v : -INFINITY; });
   }
-  for (int b = 0; b < nvec; b += kRowUnroll * kRowThreads) {
-    uint4 v[kRowUnroll];
-#pragma unroll
-    for (int q = 0; q < kRowUnroll; ++q) {
-      const int i = b + q * kRowThreads + tid;
-      v[q] = i < nvec ? __ldg(vecs + i) : make_uint4(Type::neg_inf, Type::neg_inf, Type::neg_inf, Type::neg_inf);
-    }
+  auto work = [&](const uint4 (&v)[kRowUnroll], int b) {
     float x[kRowUnroll * E], cmax = -INFINITY;
 #pragma unroll
     for (int q = 0; q < kRowUnroll; ++q) {
@@ -315,12 +325,53 @@ logits_rows_kernel(const RowsArgs args) {
       const int i = b + (j / E) * kRowThreads + tid;
       return i < nvec ? row_value(base[first_id + i * E + j % E]) : -INFINITY;
     });
+  };
+  // The slice streams through a ring of four 16 KB batches that the copy engine fills (192 KB in flight on an SM with
+  // three blocks; with the next batch in registers instead, latency showed at 4.4 TB/s).  A batch's slot is filled again
+  // one batch after it was read, by then by all warps.
+  const int n_batch = (nvec + kRowBatch - 1) / kRowBatch;
+  auto refill = [&](int i) {                                        // thread 0
+    const uint32_t bytes = (uint32_t)min(kRowBatch, nvec - i * kRowBatch) * 16u, bar = ptx::smem_u32(&bar_full[i % kRowStages]);
+    ptx::mbar_arrive_expect_tx(bar, bytes);
+    ptx::bulk_load(ring + (uint32_t)(i % kRowStages) * kRowBatch * 16u, vecs + (size_t)i * kRowBatch, bytes, bar);
+  };
+  if (tid == 0)
+    for (int i = 0; i < min(n_batch, kRowStages); ++i) refill(i);
+  for (int i = 0; i < n_batch; ++i) {
+    const int stage = i % kRowStages, b = i * kRowBatch;
+    if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(ptx::smem_u32(&bar_full[stage]), (uint32_t)(i / kRowStages) & 1u, &abort_flag,
+                                                        kWaitLimitCycles)))
+      break;
+    uint4 v[kRowUnroll];
+    const uint4* src = ring_ptr + stage * kRowBatch + tid;
+#pragma unroll
+    for (int q = 0; q < kRowUnroll; ++q) v[q] = src[q * kRowThreads];
+    if (b + kRowBatch > nvec) {                                     // the last batch
+#pragma unroll
+      for (int q = 0; q < kRowUnroll; ++q)
+        if (b + q * kRowThreads + tid >= nvec) v[q] = make_uint4(Type::neg_inf, Type::neg_inf, Type::neg_inf, Type::neg_inf);
+    }
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar_empty[stage]));
+    if (tid == 0 && i > 0 && i - 1 + kRowStages < n_batch) {
+      const int last = (i - 1) % kRowStages;
+      if (ptx::mbar_wait_bounded(ptx::smem_u32(&bar_empty[last]), (uint32_t)((i - 1) / kRowStages) & 1u, &abort_flag, kWaitLimitCycles))
+        refill(i - 1 + kRowStages);
+    }
+    __syncwarp();
+    work(v, b);
+  }
+  if (abort_flag && tid == 0) {                                     // copies that are late have a bounded time to land
+    const long long t0 = clock64();
+    while (clock64() - t0 < 20000000LL) {
+    }
   }
 
   // ---- merge lanes, then warps
   {
     const float f = fmaf(-st.delta, kLn2, 1.f);                     // back from ref to c2 m: 2^-delta
     float s = st.s * f, u = fmaf(-st.delta, st.s, st.u) * f, n = st.own;
+    if (abort_flag) s = __uint_as_float(0x7FC00000u);               // a copy that never came: the row's results are NaN
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -345,13 +396,32 @@ logits_rows_kernel(const RowsArgs args) {
   if (k > 0) {
     const bool holds = tid < nvec || tid < extras;
     const uint32_t mine = holds ? (order_key(st.lane_max) >> kShift) : 0u;
-    uint32_t tau = 0u;                                              // largest class with at least k lane maxima in or above it
+    // tau: the largest class with at least k lane maxima in or above it.  One warp finds it two bits at a time, eight
+    // maxima a lane; the three counts of a round travel in one sum.
+    uint32_t* maxima = reinterpret_cast<uint32_t*>(cand);
+    maxima[tid] = mine;
+    __syncthreads();
+    if (warp == 0) {
+      uint32_t key[kWarps], found = 0u;
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) key[j] = maxima[j * 32 + lane];
+      constexpr int kTopBit = (Type::key_bits + 1) / 2 * 2 - 2;
 #pragma unroll 1
-    for (int bit = 31 - kShift; bit >= 0; --bit) {
-      const uint32_t c = tau | (1u << bit);
-      if (__syncthreads_count(mine >= c) >= k) tau = c;
+      for (int bit = kTopBit; bit >= 0; bit -= 2) {
+        const uint32_t c1 = found | (1u << bit), c2k = found | (2u << bit), c3 = found | (3u << bit);
+        uint32_t counts = 0u;
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j)
+          counts += (key[j] >= c1 ? 1u : 0u) + (key[j] >= c2k ? 1u << 10 : 0u) + (key[j] >= c3 ? 1u << 20 : 0u);
+        counts = __reduce_add_sync(0xffffffffu, counts);
+        if ((int)(counts >> 20) >= k) found = c3;
+        else if ((int)((counts >> 10) & 1023u) >= k) found = c2k;
+        else if ((int)(counts & 1023u) >= k) found = c1;
+      }
+      if (lane == 0) sh_tau = max(found, 1u);                       // 0 is NaN's class
     }
-    tau = max(tau, 1u);                                             // 0 is NaN's class
+    __syncthreads();
+    const uint32_t tau = sh_tau;
     if (mine >= tau) owners[atomicAdd(&n_owner, 1)] = tid;
     if (tid < kMaxTop) sh_mine.top[tid] = 0ull;
     __syncthreads();
@@ -364,6 +434,7 @@ logits_rows_kernel(const RowsArgs args) {
       }
     };
     // entries of class `least` or above, from the lanes whose maximum is
+    const bool in_ring = n_batch <= kRowStages;                     // a short slice is still in shared memory
     auto collect = [&](uint32_t least) {
       if (tid < extras && mine >= least) offer(row_value(base[extra_id(tid)]), extra_id(tid), least);
       const int items = n_owner * per_lane;
@@ -371,7 +442,7 @@ logits_rows_kernel(const RowsArgs args) {
         const int i = (w % per_lane) * kRowThreads + owners[w / per_lane];
         if (i >= nvec) continue;
         float x[E];
-        Type::entries(__ldg(vecs + i), x);
+        Type::entries(in_ring ? ring_ptr[i] : __ldg(vecs + i), x);
 #pragma unroll
         for (int j = 0; j < E; ++j) offer(x[j], first_id + i * E + j, least);
       }

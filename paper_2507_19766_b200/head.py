@@ -106,7 +106,7 @@ def _on(device: int):
 
 
 def _stream(device: int) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def head_workspace_bytes(p: HeadParams, backward: bool = True) -> int:
