@@ -229,19 +229,36 @@ struct RowSlice {
   unsigned long long top[kMaxTop];
 };
 
-// Adds (m, s, u) of n maxima that are not in s to the sums relative to M >= m.
-__device__ __forceinline__ void add_slice(float m, float s, float u, int n, float c2, float M, float& r, float& uu, int& owners) {
-  if (m == M) {
-    r += s;
-    uu += u;
-    owners += n;
+// The statistics that the lanes of a warp hold, together, in every lane: (m, s, u) with n entries equal to m that are
+// not in s.  Of the result's maximum one entry is not in r (owners = 1), if there is any.
+struct RowSums {
+  float m, r, u;
+  int owners;
+};
+__device__ __forceinline__ RowSums merge_lanes(float m, float s, float u, int n, float c2) {
+  RowSums o;
+  o.m = m;
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) o.m = fmaxf(o.m, __shfl_xor_sync(0xffffffffu, o.m, w));
+  o.r = s;                                                          // nothing, or the NaN that a NaN entry left
+  o.u = 0.f;
+  o.owners = 0;
+  if (m == o.m) {
+    o.u = u;
+    o.owners = n;
   } else if (m > -INFINITY) {
-    const float d = fmaxf((m - M) * c2, -1000.f), sc = fast_ex2(d), tot = s + (float)n;
-    r = fmaf(tot, sc, r);
-    uu = fmaf(sc, fmaf(d, tot, u), uu);
-  } else {
-    r += s;                                                         // nothing, or the NaN that a NaN entry left
+    const float d = fmaxf((m - o.m) * c2, -1000.f), sc = fast_ex2(d), tot = s + (float)n;
+    o.r = tot * sc;
+    o.u = sc * fmaf(d, tot, u);
   }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) {
+    o.r += __shfl_xor_sync(0xffffffffu, o.r, w);
+    o.u += __shfl_xor_sync(0xffffffffu, o.u, w);
+    o.owners += __shfl_xor_sync(0xffffffffu, o.owners, w);
+  }
+  if (o.owners > 1) { o.r += (float)(o.owners - 1); o.owners = 1; }
+  return o;
 }
 
 // A row is read once, by one block or, where there are fewer rows than the GPU takes, by a cluster of up to 16 that
@@ -265,8 +282,7 @@ logits_rows_kernel(const RowsArgs args) {
   __shared__ __align__(8) uint64_t bar_full[kRowStages], bar_empty[kRowStages];
   __shared__ volatile int abort_flag;
   __shared__ RowSlice sh_mine;
-  __shared__ float all_m[kRowMaxCluster], all_r[kRowMaxCluster], all_u[kRowMaxCluster];
-  __shared__ int all_n[kRowMaxCluster];
+  __shared__ float all_m, all_r, all_u;
   __shared__ float sh_row[2];                                       // m, ln s
   __shared__ uint32_t sh_tau;
   __shared__ unsigned long long cand[kRowCandidates];
@@ -304,6 +320,14 @@ logits_rows_kernel(const RowsArgs args) {
     ptx::fence_async_proxy();
   }
   __syncthreads();
+
+  // the target's logit is on its way early
+  int y = 0;
+  float at_y = 0.f;
+  if (tid == 0 && slice == 0 && args.logp) {
+    y = args.targets[row];
+    at_y = row_value(base[min(max(y, 0), V - 1)]);
+  }
 
   RowState st;
   if (slice == 0) {
@@ -382,61 +406,65 @@ logits_rows_kernel(const RowsArgs args) {
   }
   if (tid == 0) { n_owner = 0; n_cand = 0; }
   __syncthreads();
-  if (tid == 0) {
-    RowSlice& o = sh_mine;
-    o.m = -INFINITY;
-    for (int w = 0; w < kWarps; ++w) o.m = fmaxf(o.m, sh_m[w]);
-    o.r = o.u = 0.f;
-    o.owners = 0;
-    for (int w = 0; w < kWarps; ++w) add_slice(sh_m[w], sh_s[w], sh_u[w], sh_n[w], c2, o.m, o.r, o.u, o.owners);
-    if (o.owners > 1) { o.r += (float)(o.owners - 1); o.owners = 1; }
+  if (warp == 0) {
+    const bool on = lane < kWarps;
+    const RowSums all = merge_lanes(on ? sh_m[lane] : -INFINITY, on ? sh_s[lane] : 0.f, on ? sh_u[lane] : 0.f, on ? sh_n[lane] : 0, c2);
+    if (lane == 0) { sh_mine.m = all.m; sh_mine.r = all.r; sh_mine.u = all.u; sh_mine.owners = all.owners; }
   }
 
   // ---- the slice's k largest, falling, into sh_mine.top
   if (k > 0) {
     const bool holds = tid < nvec || tid < extras;
     const uint32_t mine = holds ? (order_key(st.lane_max) >> kShift) : 0u;
-    // tau: the largest class with at least k lane maxima in or above it.  One warp finds it two bits at a time, eight
-    // maxima a lane; the three counts of a round travel in one sum.
-    uint32_t* maxima = reinterpret_cast<uint32_t*>(cand);
-    maxima[tid] = mine;
-    __syncthreads();
-    if (warp == 0) {
-      uint32_t key[kWarps], found = 0u;
+    // The lanes' places by their maxima: each warp sorts its 32 (shuffles), and every entry then looks up in the other
+    // warps' sorted lists how many are before it.  (A search over the bits of the k-th is a chain of 8 to 16 votes:
+    // 4700 cycles with 32-bit keys.)  The lane in place k - 1 has tau, the k-th largest class.
+    uint32_t* sorted = reinterpret_cast<uint32_t*>(cand);
+    unsigned long long mine_at = ((unsigned long long)mine << 32) | (uint32_t)tid;      // falling by key
 #pragma unroll
-      for (int j = 0; j < kWarps; ++j) key[j] = maxima[j * 32 + lane];
-      constexpr int kTopBit = (Type::key_bits + 1) / 2 * 2 - 2;
-#pragma unroll 1
-      for (int bit = kTopBit; bit >= 0; bit -= 2) {
-        const uint32_t c1 = found | (1u << bit), c2k = found | (2u << bit), c3 = found | (3u << bit);
-        uint32_t counts = 0u;
+    for (int size = 2; size <= 32; size <<= 1)
 #pragma unroll
-        for (int j = 0; j < kWarps; ++j)
-          counts += (key[j] >= c1 ? 1u : 0u) + (key[j] >= c2k ? 1u << 10 : 0u) + (key[j] >= c3 ? 1u << 20 : 0u);
-        counts = __reduce_add_sync(0xffffffffu, counts);
-        if ((int)(counts >> 20) >= k) found = c3;
-        else if ((int)((counts >> 10) & 1023u) >= k) found = c2k;
-        else if ((int)(counts & 1023u) >= k) found = c1;
+      for (int step = size >> 1; step > 0; step >>= 1) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, mine_at, step);
+        const bool larger_here = ((lane & size) == 0) == ((lane & step) == 0);
+        mine_at = (other > mine_at) == larger_here ? other : mine_at;
       }
-      if (lane == 0) sh_tau = max(found, 1u);                       // 0 is NaN's class
-    }
+    const uint32_t key = (uint32_t)(mine_at >> 32);
+    sorted[tid] = key;
     __syncthreads();
-    const uint32_t tau = sh_tau;
-    if (mine >= tau) owners[atomicAdd(&n_owner, 1)] = tid;
+    int place = lane;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      // the number of entries before this one: larger ones, and equal ones of the warps before
+      int lo = 0;
+#pragma unroll
+      for (int step = 16; step > 0; step >>= 1) {
+        const uint32_t o = sorted[w * 32 + lo + step - 1];
+        if (o > key || (o == key && w < warp)) lo += step;
+      }
+      const uint32_t o = sorted[w * 32 + lo];                       // 31 compared so far
+      if (o > key || (o == key && w < warp)) ++lo;
+      if (w != warp) place += lo;
+    }
+    if (place == k - 1) sh_tau = max(key, 1u);                      // 0 is NaN's class
     if (tid < kMaxTop) sh_mine.top[tid] = 0ull;
     __syncthreads();
+    const uint32_t tau = sh_tau;
+    if (key >= tau) owners[place] = (int)(uint32_t)mine_at;         // places 0, 1, ...
+    const int n_above = __syncthreads_count(key >= tau);
+    if (tid == 0) n_owner = n_above;
+    __syncthreads();
     const int per_lane = (nvec + kRowThreads - 1) / kRowThreads;
-    auto offer = [&](float x, int id, uint32_t least) {
-      const uint32_t key = order_key(x);
-      if ((key >> kShift) >= least) {
-        const int at = atomicAdd(&n_cand, 1);
-        if (at < kRowCandidates) cand[at] = pack_entry(key, id);
-      }
+    auto offer = [&](float x, int id) {
+      const int at = atomicAdd(&n_cand, 1);
+      if (at < kRowCandidates) cand[at] = pack_entry(order_key(x), id);
     };
     // entries of class `least` or above, from the lanes whose maximum is
     const bool in_ring = n_batch <= kRowStages;                     // a short slice is still in shared memory
     auto collect = [&](uint32_t least) {
-      if (tid < extras && mine >= least) offer(row_value(base[extra_id(tid)]), extra_id(tid), least);
+      // values of the class or above, and only they, are not below it (keys up to that of -inf are nobody's)
+      const float bar = (least << kShift) <= kKeyNegInf ? -INFINITY : key_value(least << kShift);
+      if (tid < extras && row_value(base[extra_id(tid)]) >= bar) offer(row_value(base[extra_id(tid)]), extra_id(tid));
       const int items = n_owner * per_lane;
       for (int w = tid; w < items; w += kRowThreads) {
         const int i = (w % per_lane) * kRowThreads + owners[w / per_lane];
@@ -444,7 +472,8 @@ logits_rows_kernel(const RowsArgs args) {
         float x[E];
         Type::entries(in_ring ? ring_ptr[i] : __ldg(vecs + i), x);
 #pragma unroll
-        for (int j = 0; j < E; ++j) offer(x[j], first_id + i * E + j, least);
+        for (int j = 0; j < E; ++j)
+          if (x[j] >= bar) offer(x[j], first_id + i * E + j);
       }
       __syncthreads();
     };
@@ -459,7 +488,7 @@ logits_rows_kernel(const RowsArgs args) {
       __syncthreads();
       if (tid == 0) { n_cand = 0; n_owner = 0; }
       __syncthreads();
-      if (mine > tau) owners[atomicAdd(&n_owner, 1)] = tid;
+      if (key > tau) owners[atomicAdd(&n_owner, 1)] = (int)(uint32_t)mine_at;
       __syncthreads();
       collect(tau + 1u);
       if (n_cand <= kRowCandidates - k) {
@@ -468,9 +497,8 @@ logits_rows_kernel(const RowsArgs args) {
         int have = n_cand;
         for (int b = 0; b < n_local && have < k; b += kRowThreads) {
           const int id = b + tid < n_local ? local_id(b + tid) : -1;
-          uint32_t key = 0u;
-          if (id >= 0) key = order_key(row_value(base[id]));
-          const bool hit = id >= 0 && (key >> kShift) == tau;
+          const uint32_t at_id = id >= 0 ? order_key(row_value(base[id])) : 0u;
+          const bool hit = id >= 0 && (at_id >> kShift) == tau;
           const uint32_t votes = __ballot_sync(0xffffffffu, hit);
           if (lane == 0) sh_scan[warp] = __popc(votes);
           __syncthreads();
@@ -480,7 +508,7 @@ logits_rows_kernel(const RowsArgs args) {
             total += sh_scan[w];
           }
           const int at = have + before + __popc(votes & ((1u << lane) - 1u));
-          if (hit && at < k) cand[at] = pack_entry(key, id);
+          if (hit && at < k) cand[at] = pack_entry(at_id, id);
           have = min(k, have + total);
           __syncthreads();
         }
@@ -504,8 +532,8 @@ logits_rows_kernel(const RowsArgs args) {
         unsigned long long best = 0ull;
         for (int i = tid; i < n_local; i += kRowThreads) {
           const int id = local_id(i);
-          const uint32_t key = order_key(row_value(base[id]));
-          const unsigned long long e = key ? pack_entry(key, id) : 0ull;
+          const uint32_t at_id = order_key(row_value(base[id]));
+          const unsigned long long e = at_id ? pack_entry(at_id, id) : 0ull;
           if (e < last && e > best) best = e;
         }
         __syncthreads();
@@ -526,25 +554,18 @@ logits_rows_kernel(const RowsArgs args) {
   if (n_slice > 1) {
     cluster.sync();
     for (int i = tid; i < n_slice * k; i += kRowThreads) cand[i] = cluster.map_shared_rank(&sh_mine, i / k)->top[i % k];
-    if (tid < n_slice) {
-      const RowSlice* o = cluster.map_shared_rank(&sh_mine, tid);
-      all_m[tid] = o->m; all_r[tid] = o->r; all_u[tid] = o->u; all_n[tid] = o->owners;
+    if (warp == 0) {
+      const RowSlice* o = cluster.map_shared_rank(&sh_mine, lane < n_slice ? lane : 0);
+      const bool on = lane < n_slice;
+      const RowSums all = merge_lanes(on ? o->m : -INFINITY, on ? o->r : 0.f, on ? o->u : 0.f, on ? o->owners : 0, c2);
+      if (lane == 0) { all_m = all.m; all_r = all.r; all_u = all.u; }
     }
     if (tid < kMaxTop) sh_rank[tid] = 0;
     cluster.barrier_arrive();                                       // done with the other blocks' memory
     __syncthreads();
   }
   if (tid == 0) {
-    float M = sh_mine.m, r = sh_mine.r, uu = sh_mine.u;
-    int n = sh_mine.owners;
-    if (n_slice > 1) {
-      M = -INFINITY;
-      for (int j = 0; j < n_slice; ++j) M = fmaxf(M, all_m[j]);
-      r = uu = 0.f;
-      n = 0;
-      for (int j = 0; j < n_slice; ++j) add_slice(all_m[j], all_r[j], all_u[j], all_n[j], c2, M, r, uu, n);
-    }
-    if (n > 1) r += (float)(n - 1);
+    const float M = n_slice > 1 ? all_m : sh_mine.m, r = n_slice > 1 ? all_r : sh_mine.r, uu = n_slice > 1 ? all_u : sh_mine.u;
     const bool nothing = M == -INFINITY && r == 0.f;                // no entry has a probability
     const float ln_s = nothing ? 0.f : (M == -INFINITY ? __uint_as_float(0x7FC00000u) : log1pf(r));
     sh_row[0] = M;
@@ -555,15 +576,11 @@ logits_rows_kernel(const RowsArgs args) {
       if (args.norm) args.norm[row] = make_float2(M, ln_s);
       if (args.entropy) args.entropy[row] = nothing ? 0.f : max_nan(ln_s - kLn2 * uu / (1.f + r), 0.f);
       if (args.logp) {
-        int y = args.targets[row];
         const bool bad = y < 0 || y >= V;
-        if (bad && args.status) {                                   // the LM-head calls report and clamp
-          atomicOr(args.status, kStatusBadTarget);
-          y = y < 0 ? 0 : V - 1;
-        }
+        if (bad && args.status) atomicOr(args.status, kStatusBadTarget);      // the LM-head calls report and clamp
         args.logp[row] = bad && !args.status ? __uint_as_float(0x7FC00000u)
                          : nothing           ? -INFINITY
-                                             : args.kappa * (row_value(base[y]) - M) - ln_s;
+                                             : args.kappa * (at_y - M) - ln_s;
       }
     }
   }

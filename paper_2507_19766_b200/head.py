@@ -197,38 +197,41 @@ def token_scores_bwd(p: HeadParams, hidden, W, targets, scores: ScoresOut, d_log
 def logits_scores(logits: torch.Tensor, targets=None, top_k: int = 0, inv_temperature: float = 1.0,
                   out: Optional[ScoresOut] = None) -> ScoresOut:
     """ulorl_logits_scores: scores from logits [T, V] (float32, bfloat16 or float16; rows may be strided)."""
+    # a decoding step's call is mostly what the host does: few allocations, no more checks than the kernel needs
     lib = load_library()
     device = _device_of(logits, "logits")
     code = _LOGITS.get(logits.dtype)
     if code is None or logits.dim() != 2 or logits.shape[1] == 0:
         raise UlorlError("logits: expected float32, bfloat16 or float16 [T, V]")
     T, V = logits.shape
-    ld = logits.stride(0) if T > 1 else V
-    if (V > 1 and logits.stride(1) != 1) or ld < V:
+    ld, step = logits.stride()
+    if T <= 1:
+        ld = V
+    if (V > 1 and step != 1) or ld < V:
         raise UlorlError("logits: a row must be contiguous and rows must not overlap")
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return logits_scores(logits, targets, top_k, inv_temperature, out)
+    f32, k = torch.float32, top_k
     pt = _take(targets, "targets", torch.int32, T, device, optional=True)
-    k = top_k
-    with _on(device):
-        if out is None:
-            # one allocation for all outputs: a decoding step's call is mostly what the host does
-            flat = torch.empty(T * (3 + 2 * max(k, 0)), dtype=torch.float32, device=logits.device)
-            at = flat.data_ptr()
-            ptrs = (at if pt is not None else None, at + 4 * T, at + 8 * T) + ((at + 12 * T, at + 4 * T * (3 + k)) if k > 0 else (None, None))
-            code = lib.ulorl_logits_scores(logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt, *ptrs, _stream(device))
-            if k > 0:
-                logp, entropy, lse, ids, top_logp = flat.split((T, T, T, T * k, T * k))
-                out = ScoresOut(logp if pt is not None else None, entropy, lse, None, ids.view(torch.int32).view(T, k),
-                                top_logp.view(T, k))
-            else:
-                logp, entropy, lse = flat.split((T, T, T))
-                out = ScoresOut(logp if pt is not None else None, entropy, lse, None, None, None)
-        else:
-            f32 = torch.float32
-            code = lib.ulorl_logits_scores(
-                logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
-                _take(out.logp, "logp", f32, T, device, targets is None), _take(out.entropy, "entropy", f32, T, device, True),
-                _take(out.lse, "lse", f32, T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k <= 0),
-                _take(out.top_logp, "top_logp", f32, T * k, device, k <= 0), _stream(device))
+    if out is None:
+        logp, entropy, lse = torch.empty((3, T), dtype=f32, device=logits.device).unbind(0)
+        ids = top_logp = None
+        if k > 0:
+            ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+            top_logp = torch.empty((T, k), dtype=f32, device=logits.device)
+        if pt is None:
+            logp = None
+        code = lib.ulorl_logits_scores(logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
+                                       None if pt is None else logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                                       ids.data_ptr() if k > 0 else None, top_logp.data_ptr() if k > 0 else None, _stream(device))
+        out = ScoresOut(logp, entropy, lse, None, ids, top_logp)
+    else:
+        code = lib.ulorl_logits_scores(
+            logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
+            _take(out.logp, "logp", f32, T, device, targets is None), _take(out.entropy, "entropy", f32, T, device, True),
+            _take(out.lse, "lse", f32, T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k <= 0),
+            _take(out.top_logp, "top_logp", f32, T * k, device, k <= 0), _stream(device))
     if code != OK:
         _raise(code, "ulorl_logits_scores")
     return out
