@@ -138,7 +138,7 @@ struct RowsArgs {
 constexpr int kRowThreads = 256;
 constexpr int kRowUnroll = 4;          // 16-byte vectors of a thread in a batch
 constexpr int kRowBatch = kRowUnroll * kRowThreads;       // vectors: 16 KB
-constexpr int kRowStages = 4;          // batches on their way or waiting in shared memory
+constexpr int kRowStages = 3;          // batches on their way or waiting in shared memory
 constexpr size_t kRowSmem = (size_t)kRowStages * kRowBatch * 16 + 128;
 constexpr int kRowCandidates = 512;
 constexpr int kRowMaxCluster = 16;
@@ -267,7 +267,7 @@ __device__ __forceinline__ RowSums merge_lanes(float m, float s, float u, int n,
 // 256 lane maxima bounds the k-th largest entry of the slice from below, and entries at or above it sit in lanes whose
 // maximum is: only their few vectors are read again.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 3)
+__global__ void __launch_bounds__(kRowThreads, 4)
 logits_rows_kernel(const RowsArgs args) {
   namespace cg = cooperative_groups;
   using Type = RowType<T>;
@@ -350,9 +350,8 @@ logits_rows_kernel(const RowsArgs args) {
       return i < nvec ? row_value(base[first_id + i * E + j % E]) : -INFINITY;
     });
   };
-  // The slice streams through a ring of four 16 KB batches that the copy engine fills (192 KB in flight on an SM with
-  // three blocks; with the next batch in registers instead, latency showed at 4.4 TB/s).  A batch's slot is filled again
-  // one batch after it was read, by then by all warps.
+  // The slice streams through a ring of three 16 KB batches that the copy engine fills (192 KB in flight on an SM with
+  // four blocks).  A batch's slot is filled again one batch after it was read, by then by all warps.
   const int n_batch = (nvec + kRowBatch - 1) / kRowBatch;
   auto refill = [&](int i) {                                        // thread 0
     const uint32_t bytes = (uint32_t)min(kRowBatch, nvec - i * kRowBatch) * 16u, bar = ptx::smem_u32(&bar_full[i % kRowStages]);
