@@ -72,21 +72,21 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   if (pl.tensor && !pl.small) {
     // As for the policy loss: enough splits that the live hidden tiles stay in L2, then the count with the shortest
     // modelled time, waves of units x time of a unit, the fewest splits within one percent.  A unit's time is that
-    // of its contractions (8 H cycles a tile) or that of its epilogue, whichever is longer: about 2400 cycles a tile
-    // and, with alternatives, the entries that enter a row's list, k (1 + ln(columns / k)) of them, some 2.5 times as
-    // many insertions for the warp's 32 rows together.  A list starts anew in every split, so short splits pay most:
-    // 1537 tokens x 32768 entries, H 1024, k 8: 251 us with 64 splits of two tiles.
-    const double insertion = 1.5 * (p->top_k <= 8 ? 80.0 : 250.0);
+    // of its tiles, contraction (8 H cycles a tile) or epilogue, whichever is longer, and, with alternatives, that of
+    // its first tiles, where the lists fill faster than the contraction hides (two accumulators are not enough of a
+    // cushion): measured 12000 cycles a unit with lists of 8, 105000 with lists of 32 (8192 tokens x 151936, H 2048,
+    // 30 splits: 4.47, 4.62 and 5.84 million cycles without alternatives, with 8 and with 32).  Without lists every further
+    // split is still a pass over W more: 4.52 ms with 30 splits, 3.8 with 9, under the power cap.
     const int list = p->top_k <= 0 ? 0 : (p->top_k <= 8 ? 8 : kMaxTop);
+    const double tile = std::max(8.0 * H, list == 0 ? 5300.0 : (list == 8 ? 6000.0 : 7000.0));
+    const double fill = list == 0 ? 10000.0 : (list == 8 ? 12000.0 : 105000.0);
     const size_t live_bytes = (size_t)pl.workers * (size_t)tile_m * (size_t)H * 2;
     const int s_max = std::min(kHeadMaxSplits, n_tiles);
     const int s_min = std::max(1, std::min((int)((live_bytes + kStatsHiddenBudget - 1) / kStatsHiddenBudget), s_max));
     auto cost_of = [&](int s) {
       const int tps = (n_tiles + s - 1) / s;
       const int s_eff = (n_tiles + tps - 1) / tps;
-      const double columns = std::min((double)tps * kBN, (double)V);
-      const double enters = list ? list * (1.0 + std::log(std::max(1.0, columns / list))) : 0.0;
-      const double unit = std::max(tps * 8.0 * H, tps * 4000.0 + enters * insertion);
+      const double unit = tps * tile + fill;
       return (double)(((long)m_tiles * s_eff + pl.workers - 1) / pl.workers) * unit;
     };
     double best = cost_of(s_min);

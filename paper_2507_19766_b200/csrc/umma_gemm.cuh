@@ -597,7 +597,14 @@ __device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int
             uint32_t* pub = args.top_pub + grow;
             const bool mine = 2 * split + half < n_pub;
             if (mine) publish_key(pub + (size_t)(2 * split + half) * args.T_total, list.noted(q_pub - 1));
-            const uint32_t least = least_key(pub, n_pub, args.T_total);
+            uint32_t least = least_key(pub, n_pub, args.T_total);
+            // the lists of a row start together: the others' first words are worth a short wait (and only that, nothing
+            // depends on them)
+            if (n_tile == n_begin)
+              for (int q = 0; q < 8 && least == 0u; ++q) {
+                __nanosleep(100);
+                least = least_key(pub, n_pub, args.T_total);
+              }
             // entries that equal the bound may be needed (the lower id wins), those below it are not
             if (least != 0u) list.bar = fmaxf(list.bar, value_below(least));
           }
