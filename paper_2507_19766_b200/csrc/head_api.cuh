@@ -19,6 +19,7 @@ struct HeadPlan {
   size_t dz_ld, logits_ld;
   bool dw_direct;                          // d_W leaves the contraction as bf16: one panel, nothing to add to
   bool dw_acc;                             // d_W summed in float32 in the workspace, rounded at the end
+  int dh_acc, dw_acc_tiles;                // accumulators per unit of the two gradient contractions
   int dh_parts, dh_part_blocks, dh_part_rows;
   // forward scratch
   size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_top_pub, off_sorted, off_slots, off_list_z, off_logits, fwd_total;
@@ -112,11 +113,20 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   // d_hidden: few token tiles make few units (256 x 512 outputs each), so the vocabulary is cut into parts until
   // the units fill the GPU; the parts are float32 and added in order
   pl.dh_parts = 1;
+  // Units of 256 x 512 outputs load the row operand once for both halves but cannot hide their epilogue behind the next
+  // unit; units of 256 x 256 can.  d_hidden reduces over the vocabulary and its epilogue is small: 512, unless a
+  // quarter or more of the columns would be padding.  d_W reduces over the panel's tokens; measured with 512 and with
+  // 256 columns, at 151936 x 2048: 64 tokens 184 and 216 us, 200 tokens 282 and 292, 2011 tokens 1072 and 980, 8192 tokens
+  // 3990 and 3750; 50000 x 256, 2000 tokens: 74 and 51.
+  const size_t h1 = align_up((size_t)H, kBN), h2 = align_up((size_t)H, 2 * kBN);
+  pl.dh_acc = 4 * h2 >= 5 * h1 ? 1 : 2;
+  pl.dw_acc_tiles = panel > 512 || 4 * h2 >= 5 * h1 ? 1 : 2;
   if (pl.tensor) {
-    const int k_blocks = (V + kBK - 1) / kBK;
-    const int units = ((panel + tile_m - 1) / tile_m) * ((H + 2 * kBN - 1) / (2 * kBN));
+    const int atoms = pl.dh_acc == 1 ? 2 : 1;
+    const int k_blocks = (V + kBK * atoms - 1) / (kBK * atoms);
+    const int units = ((panel + tile_m - 1) / tile_m) * ((H + pl.dh_acc * kBN - 1) / (pl.dh_acc * kBN));
     int parts = units >= pl.workers ? 1 : pl.workers / units;
-    parts = std::max(1, std::min(parts, k_blocks / 16));            // a part keeps at least 1024 vocabulary entries
+    parts = std::max(1, std::min(parts, k_blocks * atoms / 16));            // a part keeps at least 1024 vocabulary entries
     pl.dh_part_blocks = (k_blocks + parts - 1) / parts;
     pl.dh_parts = (k_blocks + pl.dh_part_blocks - 1) / pl.dh_part_blocks;
     pl.dh_part_rows = (int)align_up((size_t)panel, (size_t)tile_m);
@@ -156,7 +166,16 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
 template <int kMode>
 static int launch_pair(const HeadPlan& pl, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc,
                        const UmmaArgs& a, cudaStream_t stream) {
-  return launch_umma_impl<kMode, 2, acc_per_unit_pair<kMode>()>(ma, mb, mc, a, pl.sms, stream);
+  return launch_umma_impl<kMode, 2, 1>(ma, mb, mc, a, pl.sms, stream);
+}
+
+// The gradient contractions: units of 256 x 512 (acc = 2) or 256 x 256 outputs.
+template <int kMode>
+static int launch_grad(const HeadPlan& pl, int acc, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc,
+                       UmmaArgs a, cudaStream_t stream) {
+  a.n_tiles = (a.N + acc * kBN - 1) / (acc * kBN);
+  return acc == 2 ? launch_umma_impl<kMode, 2, 2>(ma, mb, mc, a, pl.sms, stream)
+                  : launch_umma_impl<kMode, 2, 1>(ma, mb, mc, a, pl.sms, stream);
 }
 
 // The forward sweep of hidden against W on the tensor cores; `a` carries the mode's own fields.
@@ -346,7 +365,6 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
                     (uint64_t)H, 32, kBM);
       if (st != ULORL_OK) return st;
     }
-    const int h_tiles = (H + 2 * kBN - 1) / (2 * kBN);
     for (int t0 = 0, panel = 0; t0 < T; t0 += pl.panel_tokens, ++panel) {
       const int rows = std::min(T - t0, pl.panel_tokens);
       CUtensorMap dz_out, dz_k, dz_mn;
@@ -378,7 +396,6 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       UmmaArgs b{};
       b.M = rows; b.N = H; b.K = V;
       b.m_tiles = (rows + tile_m - 1) / tile_m;
-      b.n_tiles = h_tiles;
       b.group_m = kGradRasterGroup;
       b.row0 = t0;
       b.out_ld = (size_t)H;
@@ -387,7 +404,7 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
         b.n_split = pl.dh_parts;
         b.part_blocks = pl.dh_part_blocks;
         b.part_rows = pl.dh_part_rows;
-        st = launch_pair<kModeDHiddenPart>(pl, dz_k, map_w_mn, map_parts, b, stream);
+        st = launch_grad<kModeDHiddenPart>(pl, pl.dh_acc, dz_k, map_w_mn, map_parts, b, stream);
         if (st != ULORL_OK) return st;
         const size_t n = (size_t)rows * (size_t)H;
         sum_parts_kernel<<<(unsigned)((n / 8 + 255) / 256), 256, 0, stream>>>(
@@ -395,14 +412,13 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
         ULORL_LAUNCH_CHECK();
       } else {
         b.d_hidden = static_cast<__nv_bfloat16*>(d_hidden);
-        st = launch_pair<kModeDHidden>(pl, dz_k, map_w_mn, map_w_mn, b, stream);
+        st = launch_grad<kModeDHidden>(pl, pl.dh_acc, dz_k, map_w_mn, map_w_mn, b, stream);
         if (st != ULORL_OK) return st;
       }
       // d_W[v, h] (+)= sum_m dz[m, v] hidden[t0 + m, h]
       UmmaArgs c{};
       c.M = V; c.N = H; c.K = rows;
       c.m_tiles = (V + tile_m - 1) / tile_m;
-      c.n_tiles = h_tiles;
       c.group_m = kGradRasterGroup;
       c.b_k0 = t0;
       c.d_W = d_W;
@@ -410,8 +426,8 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       c.dz_cols = H;
       c.accumulate = (panel > 0 || acc_into) ? 1 : 0;
       c.status = a.status;
-      st = pl.dw_direct ? launch_pair<kModeDWBf16>(pl, dz_mn, map_hidden_mn, map_dw, c, stream)
-                        : launch_pair<kModeDW>(pl, dz_mn, map_hidden_mn, map_dw, c, stream);
+      st = pl.dw_direct ? launch_grad<kModeDWBf16>(pl, pl.dw_acc_tiles, dz_mn, map_hidden_mn, map_dw, c, stream)
+                        : launch_grad<kModeDW>(pl, pl.dw_acc_tiles, dz_mn, map_hidden_mn, map_dw, c, stream);
       if (st != ULORL_OK) return st;
     }
   } else {

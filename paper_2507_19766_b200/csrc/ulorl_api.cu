@@ -284,7 +284,7 @@ static int launch_umma_impl(const CUtensorMap& ma, const CUtensorMap& mb, const 
                             int num_sms, cudaStream_t stream) {
   // the shared-memory opt-in is a property of the function on ONE device: set up once per device
   static bool opted_in[kMaxDevices] = {};
-  constexpr size_t smem = PipeConfig<kCta, kAcc, KAtoms<kMode, kCta>::value>::smem_bytes;
+  constexpr size_t smem = PipeConfig<kCta, kAcc, KAtoms<kMode, kCta, kAcc>::value>::smem_bytes;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return ULORL_ERR_CUDA;
   {

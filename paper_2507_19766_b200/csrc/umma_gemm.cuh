@@ -83,8 +83,8 @@ struct ModeTraits {
   static constexpr int timing_kind = sweep ? 0 : (dz ? 1 : (dh ? 2 : 3));
 };
 
-template <int kMode, int kCta>
-struct KAtoms { static constexpr int value = (kCta == 2 && (ModeTraits<kMode>::sweep || ModeTraits<kMode>::dz)) ? 2 : 1; };
+template <int kMode, int kCta, int kAcc>
+struct KAtoms { static constexpr int value = (kCta == 2 && kAcc == 1) ? 2 : 1; };
 
 template <int kCta, int kAcc, int kKA>
 struct PipeConfig {
@@ -696,7 +696,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       args.m_tiles = (n + kBM * kCta - 1) / (kBM * kCta);
     }
   }
-  constexpr int kKA = KAtoms<kMode, kCta>::value;
+  constexpr int kKA = KAtoms<kMode, kCta, kAcc>::value;
   using Cfg = PipeConfig<kCta, kAcc, kKA>;
   using Tr = ModeTraits<kMode>;
   static_assert(kAcc == 1 || (kCta == 2 && (Tr::dh || Tr::dw)), "two accumulators: gradient modes, CTA pairs");
