@@ -133,11 +133,12 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   }
   size_t off = 256;
   pl.off_status = 0;
+  pl.off_top_pub = off;   // behind the status word: cleared together
+  if (pl.tensor && !pl.small && K) off = align_up(off + sizeof(uint32_t) * (size_t)std::min(pl.n_partial, 32) * T1, 256);
   pl.off_partials = off;  off = align_up(off + sizeof(float4) * (size_t)pl.n_partial * T1, 256);
   pl.off_acc_y = off;     off = align_up(off + sizeof(float) * T1, 256);
   pl.off_top_val = off;   off = align_up(off + sizeof(float) * (size_t)pl.n_partial * T1 * K, 256);
   pl.off_top_id = off;    off = align_up(off + sizeof(int) * (size_t)pl.n_partial * T1 * K, 256);
-  pl.off_top_pub = off;   off = align_up(off + (K ? sizeof(uint32_t) * (size_t)std::min(pl.n_partial, 32) * T1 : 0), 256);
   pl.off_sorted = off;    off = align_up(off + sizeof(int) * T1 * K, 256);
   pl.off_list_z = off;    off = align_up(off + sizeof(float) * T1 * K, 256);
   pl.off_slots = off;     off = align_up(off + T1 * K, 1024);
@@ -324,13 +325,13 @@ static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   return check_launch();
 }
 
-static int head_begin(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, void* workspace,
-                      size_t workspace_bytes, size_t need, cudaStream_t stream) {
+// Checks what every call shares and clears the first `clear` bytes of the workspace (the status word; 0: a kernel does).
+static int head_begin(const void* hidden, const void* W, void* workspace, size_t workspace_bytes, size_t need, size_t clear,
+                      cudaStream_t stream) {
   if (!hidden || !W || !workspace) return ULORL_ERR_INVALID_ARG;
   if (!aligned16(hidden) || !aligned16(W) || !aligned16(workspace)) return ULORL_ERR_UNSUPPORTED;
   if (workspace_bytes < need) return ULORL_ERR_WORKSPACE;
-  (void)p;
-  if (cudaMemsetAsync(static_cast<uint8_t*>(workspace) + pl.off_status, 0, 256, stream) != cudaSuccess) return ULORL_ERR_CUDA;
+  if (clear && cudaMemsetAsync(workspace, 0, clear, stream) != cudaSuccess) return ULORL_ERR_CUDA;
   return ULORL_OK;
 }
 
@@ -504,7 +505,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
   if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
   const HeadPlan pl = make_head_plan(params);
-  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.fwd_total, stream);
+  st = head_begin(hidden, W, workspace, workspace_bytes, pl.fwd_total, pl.tensor && !pl.small && k > 0 ? pl.off_partials : 256, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   if (pl.tensor && !pl.small) {
@@ -515,8 +516,6 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
     a.top_val = reinterpret_cast<float*>(ws + pl.off_top_val);
     a.top_id = reinterpret_cast<int*>(ws + pl.off_top_id);
     a.top_pub = reinterpret_cast<uint32_t*>(ws + pl.off_top_pub);
-    if (k > 0 && cudaMemsetAsync(a.top_pub, 0, sizeof(uint32_t) * (size_t)std::min(pl.n_partial, 32) * (size_t)T, stream) != cudaSuccess)
-      return ULORL_ERR_CUDA;
     st = run_sweep(params, pl, k == 0 ? kModeScores : (k <= 8 ? kModeScoresTop8 : kModeScoresTop32), a, hidden, W, ws, stream);
     if (st != ULORL_OK) return st;
     MergeArgs m{};
@@ -568,13 +567,14 @@ int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden
   if ((d_logp && (!logp || !targets)) || (d_entropy && !entropy)) return ULORL_ERR_INVALID_ARG;
   if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
   const HeadPlan pl = make_head_plan(params);
-  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.bwd_total, stream);
+  st = head_begin(hidden, W, workspace, workspace_bytes, pl.bwd_total, 0, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float4* row_p = reinterpret_cast<float4*>(ws + pl.off_row_p);
   float* row_ins = reinterpret_cast<float*>(ws + pl.off_row_ins);
-  row_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<const float2*>(norm), logp,
-                                                         entropy, d_logp, d_entropy, row_p, row_ins);
+  row_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<int*>(ws + pl.off_status),
+                                                         reinterpret_cast<const float2*>(norm), logp, entropy, d_logp, d_entropy,
+                                                         row_p, row_ins);
   ULORL_LAUNCH_CHECK();
   return run_head_bwd(params, pl, hidden, W, d_logp ? targets : nullptr, row_p, row_ins, nullptr, d_hidden, d_W, ws, stream);
 }
@@ -618,7 +618,7 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
   if (!teacher_ids || !teacher_logp || !kl || !norm || !coef || !entry_grad) return ULORL_ERR_INVALID_ARG;
   if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
   const HeadPlan pl = make_head_plan(params);
-  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.fwd_total, stream);
+  st = head_begin(hidden, W, workspace, workspace_bytes, pl.fwd_total, 256, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   int* status = reinterpret_cast<int*>(ws + pl.off_status);
@@ -662,9 +662,9 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
   d.list_z = list_z; d.slots = slots;
   d.teacher = teacher_logp; d.weights = weights;
   d.kl = kl; d.norm = reinterpret_cast<float2*>(norm); d.lse = lse; d.coef = coef; d.entry_grad = entry_grad;
-  distill_rows_kernel<<<row_blocks, 256, 0, stream>>>(d);
-  ULORL_LAUNCH_CHECK();
-  distill_loss_kernel<<<1, 1024, 0, stream>>>(T, kl, weights, d.inv_N, loss);
+  d.loss = loss;
+  d.done = reinterpret_cast<unsigned int*>(status) + 16;            // cleared with the status word
+  distill_rows_kernel<<<row_blocks, kDistillThreads, 0, stream>>>(d);
   return check_launch();
 }
 
@@ -682,12 +682,13 @@ int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, con
   if (!teacher_ids || !norm || !coef || !entry_grad || !d_hidden || !d_W) return ULORL_ERR_INVALID_ARG;
   if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
   const HeadPlan pl = make_head_plan(params);
-  st = head_begin(params, pl, hidden, W, workspace, workspace_bytes, pl.bwd_total, stream);
+  st = head_begin(hidden, W, workspace, workspace_bytes, pl.bwd_total, 0, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float4* row_p = reinterpret_cast<float4*>(ws + pl.off_row_p);
-  distill_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<const float2*>(norm),
-                                                             coef, grad_loss, row_p);
+  distill_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature,
+                                                             reinterpret_cast<int*>(ws + pl.off_status),
+                                                             reinterpret_cast<const float2*>(norm), coef, grad_loss, row_p);
   ULORL_LAUNCH_CHECK();
   auto put_list = [&](int t0, int rows) -> int {
     const size_t n = (size_t)rows * (size_t)K;

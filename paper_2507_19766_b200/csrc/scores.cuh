@@ -784,10 +784,12 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const Me
 // ------------------------------------------------------------------------------------------ gradients of scores
 // (m, log2 s, alpha, beta) and the value at the target's column for the dz pass:
 //   dz_j = kappa g (1[j = y] - p_j) - kappa e p_j (log p_j + H) = 2^L (alpha + beta L) off the target, L = log2 p_j.
-__global__ void row_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ logp,
+// The first kernel of the backward call: it also clears the status word.
+__global__ void row_params_kernel(int T, float kappa, int* __restrict__ status, const float2* __restrict__ norm, const float* __restrict__ logp,
                                   const float* __restrict__ entropy, const float* __restrict__ d_logp,
                                   const float* __restrict__ d_entropy, float4* __restrict__ row_p, float* __restrict__ row_ins) {
   const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t == 0) *status = 0;
   if (t >= T) return;
   const float g = d_logp ? d_logp[t] : 0.f, e = d_entropy ? d_entropy[t] : 0.f;
   const float H = d_entropy ? entropy[t] : 0.f;
@@ -902,6 +904,8 @@ struct DistillRowArgs {
   float* kl;                // [T]
   float2* norm;             // [T] (m, ln s) over all entries
   float* lse;               // [T] or NULL
+  float* loss;
+  unsigned int* done;       // zero before the launch
   float* coef;              // [T]: d loss / d z_j = coef p_j off the list
   float* entry_grad;        // [T][K]: d loss / d z at the entry's id
 };
@@ -917,12 +921,12 @@ __device__ __forceinline__ double warp_max(double v) {
   return v;
 }
 
+constexpr int kDistillThreads = 256;
+
 // The loss of a token and its gradient on the list, one warp per token, in 64 bits: a token has at most 128 entries,
 // and 1 - sum q and the differences p - q cancel.
-__global__ void distill_rows_kernel(const DistillRowArgs a) {
+__device__ __forceinline__ void distill_row(const DistillRowArgs& a, int t) {
   const int lane = threadIdx.x & 31;
-  const int t = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  if (t >= a.T) return;
   constexpr int kPer = kMaxList / 32;
   float m_off, r_off, unused;
   merge_partials(a.partials, a.n_split, a.T, t, a.kappa * kLog2e, m_off, r_off, unused);
@@ -1024,28 +1028,38 @@ __global__ void distill_rows_kernel(const DistillRowArgs a) {
   }
 }
 
-// loss = 1/N sum w_t kl_t, by one block in a fixed order.
-__global__ void distill_loss_kernel(int T, const float* __restrict__ kl, const float* __restrict__ weights, double inv_N,
-                                    float* __restrict__ loss) {
-  __shared__ double part[1024];
+// The rows, and the batch loss 1/N sum w_t kl_t by the block that is done last, in a fixed order.
+__global__ void __launch_bounds__(kDistillThreads) distill_rows_kernel(const DistillRowArgs a) {
+  const int t = blockIdx.x * (kDistillThreads / 32) + (threadIdx.x >> 5);
+  if (t < a.T) distill_row(a, t);
+  __shared__ bool last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(a.done, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  __shared__ double part[kDistillThreads];
   double acc = 0.0;
-  for (int t = threadIdx.x; t < T; t += 1024) {
-    const double w = weights ? (double)weights[t] : 1.0;
-    if (w != 0.0) acc += w * (double)kl[t];
+  for (int i = threadIdx.x; i < a.T; i += kDistillThreads) {
+    const double w = a.weights ? (double)a.weights[i] : 1.0;
+    if (w != 0.0) acc += w * (double)__ldcg(a.kl + i);              // written by other blocks
   }
   part[threadIdx.x] = acc;
   __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
+  for (int o = kDistillThreads / 2; o > 0; o >>= 1) {
     if (threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
     __syncthreads();
   }
-  if (threadIdx.x == 0) *loss = (float)(part[0] * inv_N);
+  if (threadIdx.x == 0) *a.loss = (float)(part[0] * a.inv_N);
 }
 
-// Row parameters of the dz pass: dz_j = kappa grad_loss coef p_j off the list.
-__global__ void distill_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ coef,
+// Row parameters of the dz pass: dz_j = kappa grad_loss coef p_j off the list.  The first kernel of the backward call: it
+// also clears the status word.
+__global__ void distill_params_kernel(int T, float kappa, int* __restrict__ status, const float2* __restrict__ norm, const float* __restrict__ coef,
                                       const float* __restrict__ grad_loss, float4* __restrict__ row_p) {
   const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t == 0) *status = 0;
   if (t >= T) return;
   const float gl = grad_loss ? *grad_loss : 1.f;
   row_p[t] = make_float4(norm[t].x, norm[t].y * kLog2e, kappa * gl * coef[t], 0.f);
