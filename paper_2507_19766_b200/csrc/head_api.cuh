@@ -335,10 +335,11 @@ static int head_begin(const void* hidden, const void* W, void* workspace, size_t
   return ULORL_OK;
 }
 
-// dz panels and the two gradient contractions.  row_p (and row_ins, targets) say what a row of dz is; put_list
+// dz panels and the two gradient contractions.  row_p (and row_ins, targets) say what a row of dz is (flat: with beta = 0
+// in all of them); put_list
 // writes the teacher lists' columns of a panel, if there are any.
 static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W,
-                        const int32_t* targets, const float4* row_p, const float* row_ins,
+                        const int32_t* targets, const float4* row_p, const float* row_ins, bool flat,
                         const std::function<int(int, int)>& put_list, void* d_hidden, void* d_W_out, uint8_t* ws,
                         cudaStream_t stream) {
   const int T = p->T, H = p->H, V = p->V;
@@ -385,6 +386,7 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       a.targets = targets;
       a.row_p = row_p;
       a.row_ins = row_ins;
+      a.row_flat = flat ? 1 : 0;
       a.dz_cols = (int)pl.dz_ld;
       a.status = reinterpret_cast<int*>(ws + pl.off_status);
       st = launch_pair<kModeDzRow>(pl, map_hidden_k, map_w_k, dz_out, a, stream);
@@ -576,7 +578,7 @@ int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden
                                                          reinterpret_cast<const float2*>(norm), logp, entropy, d_logp, d_entropy,
                                                          row_p, row_ins);
   ULORL_LAUNCH_CHECK();
-  return run_head_bwd(params, pl, hidden, W, d_logp ? targets : nullptr, row_p, row_ins, nullptr, d_hidden, d_W, ws, stream);
+  return run_head_bwd(params, pl, hidden, W, d_logp ? targets : nullptr, row_p, row_ins, d_entropy == nullptr, nullptr, d_hidden, d_W, ws, stream);
 }
 
 int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V, int64_t ld, int32_t top_k,
@@ -701,7 +703,7 @@ int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, con
                                                      reinterpret_cast<float*>(ws + pl.off_panel), pl.dz_ld);
     return check_launch();
   };
-  return run_head_bwd(params, pl, hidden, W, nullptr, row_p, nullptr, put_list, d_hidden, d_W, ws, stream);
+  return run_head_bwd(params, pl, hidden, W, nullptr, row_p, nullptr, true, put_list, d_hidden, d_W, ws, stream);
 }
 
 }  // extern "C"

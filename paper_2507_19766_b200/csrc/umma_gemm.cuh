@@ -142,6 +142,7 @@ struct UmmaArgs {
   // kModeDzRow
   const float4* row_p;      // (m, log2 s, alpha, beta): L = c2 (a - m) - log2 s, dz = 2^L (alpha + beta L)
   const float* row_ins;     // dz at column targets[t]; read when targets is not NULL
+  int row_flat;             // beta is zero in every row
   // kModeDHiddenPart: part s covers the k-blocks [s * part_blocks, (s + 1) * part_blocks) and writes rows
   // [s * part_rows, ...) of the output map; n_split parts
   int part_blocks, part_rows;
@@ -251,22 +252,43 @@ __device__ __forceinline__ void drop_column(uint32_t (&raw)[32], int idx) {
                  : "+r"(raw[j]) : "r"(idx), "r"(j));
 }
 
-// One 32-column chunk of dz = 2^L (alpha + beta L), L = c2 (a - m) - log2 s; zero at or beyond nvalid, and for a
-// row with alpha = beta = 0 whatever its logits.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
+      "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// One 32-column chunk of dz = 2^L (alpha + beta L), L = c2 (a - m) - log2 s; zero at or beyond nvalid, and for a row that
+// is not live (alpha = beta = 0) whatever its logits.  The difference to m is taken first: at a peaked row's maximum L is
+// 10^-9, and the term is all there is to the row.
 template <bool kFull>
 __device__ __forceinline__ void dz_row_chunk(const uint32_t (&raw)[32], int nvalid, float c2, const float4& rp, bool live,
                                              uint32_t* packed) {
+  const float2 cc = make_float2(c2, c2), nm = make_float2(-rp.x, -rp.x), ns = make_float2(-rp.y, -rp.y);
+  const float2 aa = make_float2(rp.z, rp.z), bb = make_float2(rp.w, rp.w);
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {
-    float v[2] = {0.f, 0.f};
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      if (kFull || j + q < nvalid) {
-        const float L = fmaf(__uint_as_float(raw[j + q]) - rp.x, c2, -rp.y);
-        v[q] = ex2f(L) * fmaf(rp.w, L, rp.z);
-      }
-    }
-    __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+    const float2 L = fma2(add2(make_float2(__uint_as_float(raw[j]), __uint_as_float(raw[j + 1])), nm), cc, ns);
+    float2 v = mul2(make_float2(ex2f(L.x), ex2f(L.y)), fma2(bb, L, aa));
+    if (!kFull && j >= nvalid) v.x = 0.f;
+    if (!kFull && j + 1 >= nvalid) v.y = 0.f;
+    __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
     packed[j >> 1] = live ? *reinterpret_cast<uint32_t*>(&h) : 0u;
   }
 }
@@ -311,21 +333,6 @@ __device__ __forceinline__ void put_bf16(uint32_t (&packed)[32], int idx, uint32
 // With four warps and scalar arithmetic a tile of 256 x 256 took 13400 cycles (8192 tokens x 32768 entries, H 512:
 // 393 us), more than its contraction up to H = 1600.
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
-      "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
-      "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-
 // Stands for a column that does not count (beyond the vocabulary, or on a teacher's list): its exponential is zero
 // and, unlike that of -inf, so is the product with its exponent.
 constexpr float kNoColumn = -1e30f;
@@ -984,6 +991,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       }
       float k_row = -INFINITY;                          // kModeDz: log2|coef| - lse log2(e); -inf gives a zero row
       uint32_t sign_mask = 0u;
+      if (kMode == kModeDzRow && row_ok) {
+        if (rp.z != 0.f) k_row = log2f(fabsf(rp.z)) - fmaf(rp.x, c2, rp.y);
+        sign_mask = rp.z < 0.f ? 0x80008000u : 0u;
+      }
       if (kMode == kModeDz) {
         if (row_ok) {
           const float gl = args.grad_loss ? *args.grad_loss : 1.f;
@@ -1027,11 +1038,22 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
               if (nv1 >= 32) dz_chunk<true>(raw1, 32, c2, k_row, sign_mask, packed + 16);
               else dz_chunk<false>(raw1, nv1, c2, k_row, sign_mask, packed + 16);
             } else if (kMode == kModeDzRow) {
-              const bool live = rp.z != 0.f || rp.w != 0.f;
-              if (nv0 >= 32) dz_row_chunk<true>(raw0, 32, c2, rp, live, packed);
-              else dz_row_chunk<false>(raw0, nv0, c2, rp, live, packed);
-              if (nv1 >= 32) dz_row_chunk<true>(raw1, 32, c2, rp, live, packed + 16);
-              else dz_row_chunk<false>(raw1, nv1, c2, rp, live, packed + 16);
+              if (args.row_flat) {                             // beta = 0 everywhere: alpha goes into the exponent
+                if (nv0 >= 32) dz_chunk<true>(raw0, 32, c2, k_row, sign_mask, packed);
+                else dz_chunk<false>(raw0, nv0, c2, k_row, sign_mask, packed);
+                if (nv1 >= 32) dz_chunk<true>(raw1, 32, c2, k_row, sign_mask, packed + 16);
+                else dz_chunk<false>(raw1, nv1, c2, k_row, sign_mask, packed + 16);
+                if (rp.z == 0.f) {
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) packed[j] = 0u;
+                }
+              } else {
+                const bool live = rp.z != 0.f || rp.w != 0.f;
+                if (nv0 >= 32) dz_row_chunk<true>(raw0, 32, c2, rp, live, packed);
+                else dz_row_chunk<false>(raw0, nv0, c2, rp, live, packed);
+                if (nv1 >= 32) dz_row_chunk<true>(raw1, 32, c2, rp, live, packed + 16);
+                else dz_row_chunk<false>(raw1, nv1, c2, rp, live, packed + 16);
+              }
               if (row_ok && y >= col0 && y < col0 + 64) {
                 const __nv_bfloat16 hv = __float2bfloat16_rn(ins);
                 put_bf16(packed, y - col0, (uint32_t)(*reinterpret_cast<const uint16_t*>(&hv)));
