@@ -78,7 +78,8 @@ struct ModeTraits {
   static constexpr bool a_mn = dw;
   static constexpr bool b_mn = dh || dw;
   static constexpr bool wide = scores || kMode == kModeDistill;       // eight epilogue warps
-  static constexpr int epi_warps = wide ? 8 : 4;
+  static constexpr bool two_groups = (kMode == kModeDzRow || kMode == kModeDWBf16);   // two groups of four, 64 columns in turn
+  static constexpr int epi_warps = wide || two_groups ? 8 : 4;
   static constexpr int threads = 64 + 32 * epi_warps;
   static constexpr int timing_kind = sweep ? 0 : (dz ? 1 : (dh ? 2 : 3));
 };
@@ -942,6 +943,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   } else {
     // ------------------------------------------------------------------ epilogue (warps 2..5, every CTA)
     const int quarter = warp & 3;                       // tensor-memory lanes 32 * quarter ..
+    // two_groups: group 0 takes the even 64-column blocks of a tile, group 1 the odd ones, each through a staging tile
+    // and a barrier of its own; what one waits for (tensor memory, its barriers, its last copy) the other fills
+    const int group = Tr::two_groups ? (warp - 2) >> 2 : 0;
     const int row_in_tile = quarter * 32 + lane;
     const float c2 = args.kappa * 1.4426950408889634f;  // exp(kappa a) = 2^(c2 a)
     uint32_t acc_iter = 0;
@@ -1012,8 +1016,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         // The give-up decision is taken by the 128 epilogue threads together: a thread that saw the wait
         // complete while another saw the abort flag would otherwise go on alone to warp-wide tensor-memory
         // loads and to the epilogue barrier, which the others never reach.
-        if (!epilogue_all(mbar_wait_bounded<true>(smem_u32(&bar_tmem_full[buf]), buf_phase, abort_p, kWaitLimitCycles)))
-          goto role_done;
+        const bool arrived = mbar_wait_bounded<true>(smem_u32(&bar_tmem_full[buf]), buf_phase, abort_p, kWaitLimitCycles);
+        if (!(Tr::two_groups ? epilogue_group_all(group, arrived) : epilogue_all(arrived))) goto role_done;
         tc_fence_after_sync();
         const uint32_t taddr = tmem_base + buf * kUnitN + ((uint32_t)(quarter * 32) << 16);
         if (Tr::out_bf16) {
@@ -1021,9 +1025,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           // swizzled staging tile in shared memory -> one TMA store of 128 rows x 128 bytes, so that the
           // panel is written in whole lines by the copy engine instead of 16 bytes a thread
           const int tile_row = (m_tile * kCta + cta_rank) * kBM;
-          const bool issuer = (threadIdx.x == 64);             // first thread of the epilogue warps
+          const bool issuer = (threadIdx.x == 64 + 128 * group);   // first thread of the epilogue warps (of the group)
 #pragma unroll 1
-          for (int g = 0; g < kUnitN / 64; ++g) {
+          for (int g = group; g < kUnitN / 64; g += Tr::two_groups ? 2 : 1) {
             const int col0 = col_base + g * 64;
             if (col0 >= args.dz_cols) break;
             uint32_t raw0[32], raw1[32];
@@ -1074,9 +1078,14 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
               const __nv_bfloat16 hv = __float2bfloat16_rn(vy);
               put_bf16(packed, idx, (uint32_t)(*reinterpret_cast<const uint16_t*>(&hv)));
             }
-            const uint32_t out_buf = smem_base + kStagesT * kStageBytesCta + (stage_iter++ & 1u) * kOutStageBytes;
-            if (issuer) bulk_wait_read_le1();                  // the copy that last read this staging tile is done with it
-            epilogue_bar_sync();
+            const uint32_t out_buf =
+                smem_base + kStagesT * kStageBytesCta + (Tr::two_groups ? (uint32_t)group : (stage_iter++ & 1u)) * kOutStageBytes;
+            if (issuer) {                                      // the copy that last read this staging tile is done with it
+              if (Tr::two_groups) bulk_wait_read_all();
+              else bulk_wait_read_le1();
+            }
+            if (Tr::two_groups) epilogue_group_sync(group);
+            else epilogue_bar_sync();
             const uint32_t row_addr = out_buf + (uint32_t)row_in_tile * 128u;
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
@@ -1086,7 +1095,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                            : "memory");
             }
             fence_async_proxy();
-            epilogue_bar_sync();
+            if (Tr::two_groups) epilogue_group_sync(group);
+            else epilogue_bar_sync();
             if (issuer) {
               // rows past the panel's capacity (d_W: past the vocabulary) are clipped
               if (Tr::dz || tile_row < args.M) tma_store_2d(&map_c, out_buf, col0, (Tr::dz ? 0 : args.row0) + tile_row);
@@ -1164,7 +1174,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   }
 
 role_done:
-  if ((Tr::out_bf16 || Tr::out_f32) && threadIdx.x == 64) bulk_wait_all();   // the tile copies have left shared memory and landed
+  if ((Tr::out_bf16 || Tr::out_f32) && (threadIdx.x == 64 || (Tr::two_groups && threadIdx.x == 192))) bulk_wait_all();   // the tile copies have left shared memory and landed
   if (*abort_p && lane == 0) atomicOr(args.status, kStatusTimeout);
   tc_fence_before_sync();
   __syncthreads();
