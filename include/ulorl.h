@@ -371,7 +371,7 @@ typedef struct {
 
 /* Bytes of workspace of the calls below (pure host function; 0 on invalid params).  backward = 0: enough for
  * ulorl_token_scores and ulorl_distill_fwd; 1: for the backward calls as well.  Nothing in the workspace has to
- * survive from one call to the next. */
+ * survive from one call to the next; the status word is cleared by the forward calls, not by the backward ones. */
 size_t ulorl_head_workspace_bytes(const ulorl_head_params_t* params, int32_t backward);
 
 /*
@@ -421,8 +421,9 @@ int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V,
  *   loss = 1/N sum_t weights_t kl_t
  * An id that is listed twice is two entries of one event: its probabilities add in the gradient.  An id outside
  * [-1, V) is reported in the status word and left out.  Outputs: loss[1], kl[T], lse[T] (optional), and for the
- * backward call norm[T][2], coef[T] (d loss / d z_v = coef p_v off the list) and entry_grad[T][top_k] (d loss / d z at
- * the entry's id).
+ * backward call norm[T][2] (eight-byte aligned; maximum and ln sum as in ulorl_token_scores, over the entries that are
+ * not on the token's list), coef[T] (off the list d loss / d z_v = coef times the softmax of those entries) and
+ * entry_grad[T][top_k] (d loss / d z at the entry's id).
  */
 int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
                       const int32_t* teacher_ids, const float* teacher_logp, const float* weights,

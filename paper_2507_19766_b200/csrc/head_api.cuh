@@ -325,7 +325,13 @@ static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   return check_launch();
 }
 
-// Checks what every call shares and clears the first `clear` bytes of the workspace (the status word; 0: a kernel does).
+static int clear_status(void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+  if (workspace && workspace_bytes >= 256 && cudaMemsetAsync(workspace, 0, 256, stream) != cudaSuccess) return ULORL_ERR_CUDA;
+  return ULORL_OK;
+}
+
+// Checks what every call shares and clears the first `clear` bytes of the workspace: the status word, by the forward calls
+// (what they found stays there while the backward calls run).
 static int head_begin(const void* hidden, const void* W, void* workspace, size_t workspace_bytes, size_t need, size_t clear,
                       cudaStream_t stream) {
   if (!hidden || !W || !workspace) return ULORL_ERR_INVALID_ARG;
@@ -501,7 +507,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
   const int T = params->T, V = params->V, k = params->top_k;
   if (k > ULORL_MAX_TOP) return ULORL_ERR_UNSUPPORTED;
   if (k > V) return ULORL_ERR_INVALID_ARG;
-  if (T == 0) return ULORL_OK;
+  if (T == 0) return clear_status(workspace, workspace_bytes, reinterpret_cast<cudaStream_t>(cuda_stream));
   if ((k > 0) != (top_ids != nullptr) || (k > 0) != (top_logp != nullptr)) return ULORL_ERR_INVALID_ARG;
   if (logp && !targets) return ULORL_ERR_INVALID_ARG;
   if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
@@ -574,8 +580,7 @@ int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float4* row_p = reinterpret_cast<float4*>(ws + pl.off_row_p);
   float* row_ins = reinterpret_cast<float*>(ws + pl.off_row_ins);
-  row_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<int*>(ws + pl.off_status),
-                                                         reinterpret_cast<const float2*>(norm), logp, entropy, d_logp, d_entropy,
+  row_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<const float2*>(norm), logp, entropy, d_logp, d_entropy,
                                                          row_p, row_ins);
   ULORL_LAUNCH_CHECK();
   return run_head_bwd(params, pl, hidden, W, d_logp ? targets : nullptr, row_p, row_ins, d_entropy == nullptr, nullptr, d_hidden, d_W, ws, stream);
@@ -616,7 +621,10 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
   const int T = params->T, V = params->V, K = params->top_k;
   if (K < 1 || !loss) return ULORL_ERR_INVALID_ARG;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  if (T == 0) return cudaMemsetAsync(loss, 0, sizeof(float), stream) == cudaSuccess ? ULORL_OK : ULORL_ERR_CUDA;
+  if (T == 0) {
+    if (cudaMemsetAsync(loss, 0, sizeof(float), stream) != cudaSuccess) return ULORL_ERR_CUDA;
+    return clear_status(workspace, workspace_bytes, stream);
+  }
   if (!teacher_ids || !teacher_logp || !kl || !norm || !coef || !entry_grad) return ULORL_ERR_INVALID_ARG;
   if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
   const HeadPlan pl = make_head_plan(params);
@@ -688,9 +696,7 @@ int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, con
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float4* row_p = reinterpret_cast<float4*>(ws + pl.off_row_p);
-  distill_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature,
-                                                             reinterpret_cast<int*>(ws + pl.off_status),
-                                                             reinterpret_cast<const float2*>(norm), coef, grad_loss, row_p);
+  distill_params_kernel<<<(T + 255) / 256, 256, 0, stream>>>(T, params->inv_temperature, reinterpret_cast<const float2*>(norm), coef, grad_loss, row_p);
   ULORL_LAUNCH_CHECK();
   auto put_list = [&](int t0, int rows) -> int {
     const size_t n = (size_t)rows * (size_t)K;

@@ -784,12 +784,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const Me
 // ------------------------------------------------------------------------------------------ gradients of scores
 // (m, log2 s, alpha, beta) and the value at the target's column for the dz pass:
 //   dz_j = kappa g (1[j = y] - p_j) - kappa e p_j (log p_j + H) = 2^L (alpha + beta L) off the target, L = log2 p_j.
-// The first kernel of the backward call: it also clears the status word.
-__global__ void row_params_kernel(int T, float kappa, int* __restrict__ status, const float2* __restrict__ norm, const float* __restrict__ logp,
+__global__ void row_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ logp,
                                   const float* __restrict__ entropy, const float* __restrict__ d_logp,
                                   const float* __restrict__ d_entropy, float4* __restrict__ row_p, float* __restrict__ row_ins) {
   const int t = blockIdx.x * blockDim.x + threadIdx.x;
-  if (t == 0) *status = 0;
   if (t >= T) return;
   const float g = d_logp ? d_logp[t] : 0.f, e = d_entropy ? d_entropy[t] : 0.f;
   const float H = d_entropy ? entropy[t] : 0.f;
@@ -902,11 +900,11 @@ struct DistillRowArgs {
   const float* teacher;     // [T][K]
   const float* weights;     // [T] or NULL (1)
   float* kl;                // [T]
-  float2* norm;             // [T] (m, ln s) over all entries
+  float2* norm;             // [T] (m, ln s) over the entries off the list
   float* lse;               // [T] or NULL
   float* loss;
   unsigned int* done;       // zero before the launch
-  float* coef;              // [T]: d loss / d z_j = coef p_j off the list
+  float* coef;              // [T]: off the list d loss / d z_j = coef times the softmax over the entries off the list
   float* entry_grad;        // [T][K]: d loss / d z at the entry's id
 };
 
@@ -966,6 +964,8 @@ __device__ __forceinline__ void distill_row(const DistillRowArgs& a, int t) {
     if (slot[q] < 128) on += exp(kappa * ((double)z[q] - (double)top));
   on = warp_sum(on);
   const double ln_s = log(rest + on);
+  // ln of the probability off the list; from the exponents, so that it survives where rest underflows
+  const double ln_rest = m_off > -INFINITY ? kappa * ((double)m_off - (double)top) + log1p((double)r_off) - ln_s : log(rest) - ln_s;
   if (a.mode == ULORL_DISTILL_RENORM) {
     tmax = warp_max(tmax);
     const double shift = tmax > -INFINITY ? tmax : 0.0;
@@ -988,21 +988,22 @@ __device__ __forceinline__ void distill_row(const DistillRowArgs& a, int t) {
   }
   Q = warp_sum(Q);
   kl = warp_sum(kl);
-  double c_on = Q, c_off = Q;
+  // Off the list d kl / d z_j is Q p_j, in mode tail p_j - rest_q p_j / rest_p.  Both are kept as a multiple of p_j /
+  // rest_p, the softmax over what is not listed: for a student that leaves next to nothing there, p_j and rest_p
+  // underflow in float32, their quotient and the multiple do not.
+  const double rest_p = rest / (rest + on);
+  double c_on = Q, c_off = Q * rest_p;
   if (a.mode == ULORL_DISTILL_TAIL) {
     const double rest_q = fmax(1.0 - Q, 0.0);
     c_on = 1.0;
-    c_off = 1.0;
-    if (rest_q > 0.0) {
-      kl += rest_q * (log(rest_q) - (log(rest) - ln_s));
-      c_off = 1.0 - rest_q / (rest / (rest + on));
-    }
+    c_off = rest_p - rest_q;
+    if (rest_q > 0.0) kl += rest_q * (log(rest_q) - ln_rest);
   }
   const double w = a.weights ? (double)a.weights[t] : 1.0;
   const double scale = n_valid > 0 && w != 0.0 ? w * a.inv_N : 0.0;
   if (lane == 0) {
     a.kl[t] = n_valid > 0 ? (float)kl : 0.f;
-    a.norm[t] = make_float2(top, (float)ln_s);
+    a.norm[t] = m_off > -INFINITY ? make_float2(m_off, log1pf(r_off)) : make_float2(0.f, 0.f);
     if (a.lse) a.lse[t] = (float)(kappa * (double)top + ln_s);
     a.coef[t] = scale != 0.0 && (m_off > -INFINITY) ? (float)(scale * c_off) : 0.f;
   }
@@ -1054,12 +1055,10 @@ __global__ void __launch_bounds__(kDistillThreads) distill_rows_kernel(const Dis
   if (threadIdx.x == 0) *a.loss = (float)(part[0] * a.inv_N);
 }
 
-// Row parameters of the dz pass: dz_j = kappa grad_loss coef p_j off the list.  The first kernel of the backward call: it
-// also clears the status word.
-__global__ void distill_params_kernel(int T, float kappa, int* __restrict__ status, const float2* __restrict__ norm, const float* __restrict__ coef,
+// Row parameters of the dz pass: dz_j = kappa grad_loss coef softmax_j, the softmax over what is not on the list.
+__global__ void distill_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ coef,
                                       const float* __restrict__ grad_loss, float4* __restrict__ row_p) {
   const int t = blockIdx.x * blockDim.x + threadIdx.x;
-  if (t == 0) *status = 0;
   if (t >= T) return;
   const float gl = grad_loss ? *grad_loss : 1.f;
   row_p[t] = make_float4(norm[t].x, norm[t].y * kLog2e, kappa * gl * coef[t], 0.f);

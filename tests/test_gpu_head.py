@@ -129,6 +129,8 @@ def test_bad_target_is_reported_and_clamped():
         ws = U.alloc_head_workspace(p, DEV)
         out = U.token_scores(p, hidden, W, bad, workspace=ws)
         assert B.check_status(ws) == -6
+        U.token_scores_bwd(p, hidden, W, bad, out, out.logp, workspace=ws)
+        assert B.check_status(ws) == -6                       # the finding outlives the backward call
         ok = bad.clamp(0, V - 1)
         again = U.token_scores(p, hidden, W, ok, workspace=ws)
         assert B.check_status(ws) == B.OK
@@ -324,6 +326,39 @@ def test_overconfident_student_keeps_the_remainder():
         h, w = hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV)
         p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode="tail")
         check_distill(p, h, w, ids, teacher, None, dtype == "bf16")
+
+
+def test_student_that_leaves_nothing_off_the_list():
+    """Mode tail, a student whose list outweighs the rest by e^200: the rest's probability underflows in float32, its
+    logarithm and the gradient's share of it do not."""
+    T, H, V, K = 5, 64, 600, 3
+    W = torch.zeros(V, H)
+    W[torch.arange(V), torch.arange(V) % H] = 1.0
+    W[:3] *= torch.tensor([200.0, 201.0, 199.0])[:, None]
+    hidden = torch.zeros(T, H)
+    hidden[:, :3] = 1.0
+    ids = torch.arange(3, dtype=torch.int32).repeat(T, 1).to(DEV)
+    teacher = torch.log(torch.tensor([0.5, 0.3, 0.1])).repeat(T, 1).to(DEV)
+    for dtype in ("bf16", "f32"):
+        for mode in ("raw", "tail"):
+            p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode=mode)
+            out, d_h, d_W, _ = check_distill(p, hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV), ids, teacher, None, dtype == "bf16")
+            assert bool(torch.isfinite(d_h).all()) and bool(torch.isfinite(d_W).all()) and bool(torch.isfinite(out.kl).all())
+
+
+@pytest.mark.parametrize("dtype,path", [("f32", "auto"), ("bf16", "simt")])
+def test_forward_by_panels(dtype, path):
+    """The CUDA-core path's forward passes by panels of tokens: the same results as in one."""
+    T, H, V, k = 700, 64, 900, 6
+    hidden, W, targets = operands(T, H, V, dtype, seed=19)
+    ids, teacher = teacher_lists(T, V, k, seed=20)
+    one = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, kernel_path=path, distill_mode="tail")
+    many = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, kernel_path=path, distill_mode="tail", bwd_panel_tokens=200)
+    a, b = (U.token_scores(p, hidden, W, targets) for p in (one, many))
+    c, d = (U.distill_fwd(p, hidden, W, ids, teacher) for p in (one, many))
+    for x, y in ((a, b), (c, d)):
+        for name, v in vars(x).items():
+            assert torch.equal(v, getattr(y, name)), name
 
 
 # ------------------------------------------------------------------------------------------------ together
