@@ -78,7 +78,7 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
     // cushion): measured 12000 cycles a unit with lists of 8, 105000 with lists of 32 (8192 tokens x 151936, H 2048,
     // 30 splits: 4.47, 4.62 and 5.84 million cycles without alternatives, with 8 and with 32).  Without lists every further
     // split is still a pass over W more: 4.52 ms with 30 splits, 3.8 with 9, under the power cap.
-    const int list = p->top_k <= 0 ? 0 : (p->top_k <= 8 ? 8 : kMaxTop);
+    const int list = p->top_k <= 0 || p->top_k > kMaxTop ? 0 : (p->top_k <= 8 ? 8 : kMaxTop);
     const double tile = std::max(8.0 * H, list == 0 ? 5300.0 : (list == 8 ? 6000.0 : 7000.0));
     const double fill = list == 0 ? 10000.0 : (list == 8 ? 12000.0 : 105000.0);
     const size_t live_bytes = (size_t)pl.workers * (size_t)tile_m * (size_t)H * 2;
@@ -137,11 +137,14 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   if (pl.tensor && !pl.small && K) off = align_up(off + sizeof(uint32_t) * (size_t)std::min(pl.n_partial, 32) * T1, 256);
   pl.off_partials = off;  off = align_up(off + sizeof(float4) * (size_t)pl.n_partial * T1, 256);
   pl.off_acc_y = off;     off = align_up(off + sizeof(float) * T1, 256);
-  pl.off_top_val = off;   off = align_up(off + sizeof(float) * (size_t)pl.n_partial * T1 * K, 256);
-  pl.off_top_id = off;    off = align_up(off + sizeof(int) * (size_t)pl.n_partial * T1 * K, 256);
-  pl.off_sorted = off;    off = align_up(off + sizeof(int) * T1 * K, 256);
-  pl.off_list_z = off;    off = align_up(off + sizeof(float) * T1 * K, 256);
-  pl.off_slots = off;     off = align_up(off + T1 * K, 1024);
+  // the alternatives of a scoring call and the teacher lists of a distillation call are never there together
+  size_t lists = off, teacher = off;
+  pl.off_top_val = lists; lists = K <= kMaxTop ? align_up(lists + sizeof(float) * (size_t)pl.n_partial * T1 * K, 256) : lists;
+  pl.off_top_id = lists;  lists = K <= kMaxTop ? align_up(lists + sizeof(int) * (size_t)pl.n_partial * T1 * K, 256) : lists;
+  pl.off_sorted = teacher; teacher = align_up(teacher + sizeof(int) * T1 * K, 256);
+  pl.off_list_z = teacher; teacher = align_up(teacher + sizeof(float) * T1 * K, 256);
+  pl.off_slots = teacher;  teacher = align_up(teacher + T1 * K, 256);
+  off = align_up(std::max(lists, teacher), 1024);
   pl.off_logits = off;    // forward passes that go through a panel of logits
   pl.fwd_total = off;
   if (pl.small || !pl.tensor) pl.fwd_total = align_up(off + sizeof(float) * (size_t)std::min(panel, (int)T1) * pl.logits_ld, 1024);
@@ -153,8 +156,8 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   if (pl.dw_acc) { pl.off_dw_acc = off; off = align_up(off + sizeof(float) * (size_t)V * (size_t)H, 1024); }
   if (!pl.tensor && p->dtype == ULORL_F32) {      // float32 contractions cut over k
     pl.off_parts = off;
-    // tiles x parts is at most the multiprocessor count, so are the parts' rows, in tiles, of any contraction here
-    off = align_up(off + sizeof(float) * (size_t)pl.sms * kSgTile * (size_t)H, 1024);
+    // tiles x parts is at most the multiprocessor count, and a tile has no more than 128 x min(H, 128) outputs
+    off = align_up(off + sizeof(float) * (size_t)pl.sms * kSgTile * (size_t)std::min(H, kSgTile), 1024);
   }
   if (pl.dh_parts > 1) {
     pl.off_parts = off;

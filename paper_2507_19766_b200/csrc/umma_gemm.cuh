@@ -1173,7 +1173,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
   }
 
-role_done:
+[[maybe_unused]] role_done:
   if ((Tr::out_bf16 || Tr::out_f32) && (threadIdx.x == 64 || (Tr::two_groups && threadIdx.x == 192))) bulk_wait_all();   // the tile copies have left shared memory and landed
   if (*abort_p && lane == 0) atomicOr(args.status, kStatusTimeout);
   tc_fence_before_sync();
