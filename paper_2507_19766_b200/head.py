@@ -97,12 +97,9 @@ def _device_of(t: torch.Tensor, name: str) -> int:
     return t.get_device()
 
 
-_SAME = contextlib.nullcontext()
-
-
-def _on(device: int):
-    """Makes the tensors' device the current one for the call, if it is not."""
-    return _SAME if device == torch.cuda.current_device() else torch.cuda.device(device)
+def _elsewhere(device: int) -> bool:
+    """Whether the tensors' device is not the current one: the call then repeats itself with it made current."""
+    return device != torch.cuda.current_device()
 
 
 def _stream(device: int) -> int:
@@ -119,13 +116,19 @@ def head_workspace_bytes(p: HeadParams, backward: bool = True) -> int:
 def alloc_head_workspace(p: HeadParams, device, backward: bool = True) -> torch.Tensor:
     """Scratch of the calls with these params; backward=False is enough (and far smaller) for the forward ones."""
     device = torch.device(device)
-    with _SAME if device.index is None else _on(device.index):      # sizes go by the device's multiprocessor count
+    with contextlib.nullcontext() if device.index is None else torch.cuda.device(device):
+        # sizes go by the device's multiprocessor count
         return torch.empty(head_workspace_bytes(p, backward), dtype=torch.uint8, device=device)
 
 
-def _workspace(p: HeadParams, workspace, device: int, backward: bool):
+def _workspace(lib, cp: CHeadParams, workspace, hidden, device: int, backward: bool):
+    """(tensor to keep, pointer, bytes); allocates for this call where the caller keeps none."""
     if workspace is None:
-        workspace = alloc_head_workspace(p, torch.device("cuda", device), backward)
+        n = lib.ulorl_head_workspace_bytes(ctypes.byref(cp), int(backward))
+        if n == 0:
+            raise UlorlError("ulorl_head_workspace_bytes: invalid parameters")
+        workspace = torch.empty(n, dtype=torch.uint8, device=hidden.device)
+        return workspace, workspace.data_ptr(), n
     if not workspace.is_cuda or workspace.get_device() != device or not workspace.is_contiguous():
         raise UlorlError(f"workspace: expected a contiguous tensor on cuda:{device}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -137,37 +140,45 @@ def _operands(p: HeadParams, hidden, W):
     return device, _take(hidden, "hidden", dtype, p.T * p.H, device), _take(W, "W", dtype, p.V * p.H, device)
 
 
+def _alternatives(T: int, k: int, like: torch.Tensor):
+    if k <= 0:
+        return None, None
+    return (torch.empty((T, k), dtype=torch.int32, device=like.device), torch.empty((T, k), dtype=torch.float32, device=like.device))
+
+
 def token_scores(p: HeadParams, hidden, W, targets=None, out: Optional[ScoresOut] = None,
                  workspace: Optional[torch.Tensor] = None) -> ScoresOut:
     """ulorl_token_scores on the current stream of the tensors' device."""
     lib = load_library()
     cp = p.to_c()
     device, ph, pw = _operands(p, hidden, W)
-    pt = _take(targets, "targets", torch.int32, p.T, device, optional=True)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return token_scores(p, hidden, W, targets, out, workspace)
     f32, T, k = torch.float32, p.T, p.top_k
-    with _on(device):
-        if out is None:
-            rows = torch.empty(5, T, dtype=f32, device=hidden.device)
-            # norm first: pairs need eight-byte alignment
-            out = ScoresOut(rows[2] if targets is not None else None, rows[3], rows[4], rows[:2].view(T, 2),
-                            torch.empty(T, k, dtype=torch.int32, device=hidden.device) if k else None,
-                            torch.empty(T, k, dtype=f32, device=hidden.device) if k else None)
-        workspace, pws, nws = _workspace(p, workspace, device, False)
-        code = lib.ulorl_token_scores(
-            ctypes.byref(cp), ph, pw, pt, _take(out.logp, "logp", f32, T, device, targets is None),
-            _take(out.entropy, "entropy", f32, T, device, True), _take(out.lse, "lse", f32, T, device, True),
-            _take(out.norm, "norm", f32, 2 * T, device, True), _take(out.top_ids, "top_ids", torch.int32, T * k, device, k == 0),
-            _take(out.top_logp, "top_logp", f32, T * k, device, k == 0), pws, nws, _stream(device))
+    pt = _take(targets, "targets", torch.int32, T, device, optional=True)
+    if out is None:
+        logp, entropy, lse = torch.empty((3, T), dtype=f32, device=hidden.device).unbind(0)
+        out = ScoresOut(None if targets is None else logp, entropy, lse,
+                        torch.empty((T, 2), dtype=f32, device=hidden.device), *_alternatives(T, k, hidden))
+        ptrs = [None if x is None else x.data_ptr() for x in (out.logp, entropy, lse, out.norm, out.top_ids, out.top_logp)]
+    else:
+        ptrs = [_take(out.logp, "logp", f32, T, device, targets is None), _take(out.entropy, "entropy", f32, T, device, True),
+                _take(out.lse, "lse", f32, T, device, True), _take(out.norm, "norm", f32, 2 * T, device, True),
+                _take(out.top_ids, "top_ids", torch.int32, T * k, device, k == 0),
+                _take(out.top_logp, "top_logp", f32, T * k, device, k == 0)]
+    workspace, pws, nws = _workspace(lib, cp, workspace, hidden, device, False)
+    code = lib.ulorl_token_scores(ctypes.byref(cp), ph, pw, pt, *ptrs, pws, nws, _stream(device))
     if code != OK:
         _raise(code, "ulorl_token_scores")
     return out
 
 
-def _grad_outputs(p: HeadParams, d_hidden, d_W, hidden, device):
+def _grad_outputs(p: HeadParams, d_hidden, d_W, hidden, device: int):
     if d_hidden is None:
         d_hidden = torch.empty_like(hidden)
     if d_W is None:
-        d_W = (torch.zeros if p.dw_accumulate else torch.empty)(p.V, p.H, dtype=_DTYPES[p.dw_dtype], device=hidden.device)
+        d_W = (torch.zeros if p.dw_accumulate else torch.empty)((p.V, p.H), dtype=_DTYPES[p.dw_dtype], device=hidden.device)
     return (d_hidden, d_W, _take(d_hidden, "d_hidden", _DTYPES[p.dtype], p.T * p.H, device),
             _take(d_W, "d_W", _DTYPES[p.dw_dtype], p.V * p.H, device))
 
@@ -179,16 +190,18 @@ def token_scores_bwd(p: HeadParams, hidden, W, targets, scores: ScoresOut, d_log
     lib = load_library()
     cp = p.to_c()
     device, ph, pw = _operands(p, hidden, W)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return token_scores_bwd(p, hidden, W, targets, scores, d_logp, d_entropy, d_hidden, d_W, workspace)
     f32, T = torch.float32, p.T
-    with _on(device):
-        d_hidden, d_W, pdh, pdw = _grad_outputs(p, d_hidden, d_W, hidden, device)
-        workspace, pws, nws = _workspace(p, workspace, device, True)
-        code = lib.ulorl_token_scores_bwd(
-            ctypes.byref(cp), ph, pw, _take(targets, "targets", torch.int32, T, device, d_logp is None),
-            _take(scores.norm, "norm", f32, 2 * T, device), _take(scores.logp, "logp", f32, T, device, d_logp is None),
-            _take(scores.entropy, "entropy", f32, T, device, d_entropy is None),
-            _take(d_logp, "d_logp", f32, T, device, True), _take(d_entropy, "d_entropy", f32, T, device, True),
-            pdh, pdw, pws, nws, _stream(device))
+    d_hidden, d_W, pdh, pdw = _grad_outputs(p, d_hidden, d_W, hidden, device)
+    workspace, pws, nws = _workspace(lib, cp, workspace, hidden, device, True)
+    code = lib.ulorl_token_scores_bwd(
+        ctypes.byref(cp), ph, pw, _take(targets, "targets", torch.int32, T, device, d_logp is None),
+        _take(scores.norm, "norm", f32, 2 * T, device), _take(scores.logp, "logp", f32, T, device, d_logp is None),
+        _take(scores.entropy, "entropy", f32, T, device, d_entropy is None),
+        _take(d_logp, "d_logp", f32, T, device, True), _take(d_entropy, "d_entropy", f32, T, device, True),
+        pdh, pdw, pws, nws, _stream(device))
     if code != OK:
         _raise(code, "ulorl_token_scores_bwd")
     return d_hidden, d_W
@@ -209,21 +222,18 @@ def logits_scores(logits: torch.Tensor, targets=None, top_k: int = 0, inv_temper
         ld = V
     if (V > 1 and step != 1) or ld < V:
         raise UlorlError("logits: a row must be contiguous and rows must not overlap")
-    if device != torch.cuda.current_device():
+    if _elsewhere(device):
         with torch.cuda.device(device):
             return logits_scores(logits, targets, top_k, inv_temperature, out)
     f32, k = torch.float32, top_k
     pt = _take(targets, "targets", torch.int32, T, device, optional=True)
     if out is None:
         logp, entropy, lse = torch.empty((3, T), dtype=f32, device=logits.device).unbind(0)
-        ids = top_logp = None
-        if k > 0:
-            ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
-            top_logp = torch.empty((T, k), dtype=f32, device=logits.device)
-        if pt is None:
+        ids, top_logp = _alternatives(T, k, logits)
+        if targets is None:
             logp = None
         code = lib.ulorl_logits_scores(logits.data_ptr(), code, T, V, ld, k, inv_temperature, pt,
-                                       None if pt is None else logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                                       None if logp is None else logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
                                        ids.data_ptr() if k > 0 else None, top_logp.data_ptr() if k > 0 else None, _stream(device))
         out = ScoresOut(logp, entropy, lse, None, ids, top_logp)
     else:
@@ -243,21 +253,25 @@ def distill_fwd(p: HeadParams, hidden, W, teacher_ids, teacher_logp, weights=Non
     lib = load_library()
     cp = p.to_c()
     device, ph, pw = _operands(p, hidden, W)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return distill_fwd(p, hidden, W, teacher_ids, teacher_logp, weights, out, workspace)
     f32, T, k = torch.float32, p.T, p.top_k
     pi = _take(teacher_ids, "teacher_ids", torch.int32, T * k, device)
     pl = _take(teacher_logp, "teacher_logp", f32, T * k, device)
     pwt = _take(weights, "weights", f32, T, device, optional=True)
-    with _on(device):
-        if out is None:
-            rows = torch.empty(5, T, dtype=f32, device=hidden.device)
-            out = DistillOut(torch.empty(1, dtype=f32, device=hidden.device), rows[2], rows[3], rows[:2].view(T, 2), rows[4],
-                             torch.empty(T, k, dtype=f32, device=hidden.device))
-        workspace, pws, nws = _workspace(p, workspace, device, False)
-        code = lib.ulorl_distill_fwd(
-            ctypes.byref(cp), ph, pw, pi, pl, pwt, _take(out.loss, "loss", f32, 1, device), _take(out.kl, "kl", f32, T, device),
-            _take(out.lse, "lse", f32, T, device, True), _take(out.norm, "norm", f32, 2 * T, device),
-            _take(out.coef, "coef", f32, T, device), _take(out.entry_grad, "entry_grad", f32, T * k, device), pws, nws,
-            _stream(device))
+    if out is None:
+        kl, lse, coef = torch.empty((3, T), dtype=f32, device=hidden.device).unbind(0)
+        out = DistillOut(torch.empty(1, dtype=f32, device=hidden.device), kl, lse,
+                         torch.empty((T, 2), dtype=f32, device=hidden.device), coef,
+                         torch.empty((T, max(k, 0)), dtype=f32, device=hidden.device))
+        ptrs = [x.data_ptr() for x in (out.loss, kl, lse, out.norm, coef, out.entry_grad)]
+    else:
+        ptrs = [_take(out.loss, "loss", f32, 1, device), _take(out.kl, "kl", f32, T, device), _take(out.lse, "lse", f32, T, device, True),
+                _take(out.norm, "norm", f32, 2 * T, device), _take(out.coef, "coef", f32, T, device),
+                _take(out.entry_grad, "entry_grad", f32, T * k, device)]
+    workspace, pws, nws = _workspace(lib, cp, workspace, hidden, device, False)
+    code = lib.ulorl_distill_fwd(ctypes.byref(cp), ph, pw, pi, pl, pwt, *ptrs, pws, nws, _stream(device))
     if code != OK:
         _raise(code, "ulorl_distill_fwd")
     return out
@@ -269,15 +283,17 @@ def distill_bwd(p: HeadParams, hidden, W, teacher_ids, fwd: DistillOut, grad_los
     lib = load_library()
     cp = p.to_c()
     device, ph, pw = _operands(p, hidden, W)
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return distill_bwd(p, hidden, W, teacher_ids, fwd, grad_loss, d_hidden, d_W, workspace)
     f32, T, k = torch.float32, p.T, p.top_k
-    with _on(device):
-        d_hidden, d_W, pdh, pdw = _grad_outputs(p, d_hidden, d_W, hidden, device)
-        workspace, pws, nws = _workspace(p, workspace, device, True)
-        code = lib.ulorl_distill_bwd(
-            ctypes.byref(cp), ph, pw, _take(teacher_ids, "teacher_ids", torch.int32, T * k, device),
-            _take(fwd.norm, "norm", f32, 2 * T, device), _take(fwd.coef, "coef", f32, T, device),
-            _take(fwd.entry_grad, "entry_grad", f32, T * k, device), _take(grad_loss, "grad_loss", f32, 1, device, True),
-            pdh, pdw, pws, nws, _stream(device))
+    d_hidden, d_W, pdh, pdw = _grad_outputs(p, d_hidden, d_W, hidden, device)
+    workspace, pws, nws = _workspace(lib, cp, workspace, hidden, device, True)
+    code = lib.ulorl_distill_bwd(
+        ctypes.byref(cp), ph, pw, _take(teacher_ids, "teacher_ids", torch.int32, T * k, device),
+        _take(fwd.norm, "norm", f32, 2 * T, device), _take(fwd.coef, "coef", f32, T, device),
+        _take(fwd.entry_grad, "entry_grad", f32, T * k, device), _take(grad_loss, "grad_loss", f32, 1, device, True),
+        pdh, pdw, pws, nws, _stream(device))
     if code != OK:
         _raise(code, "ulorl_distill_bwd")
     return d_hidden, d_W
