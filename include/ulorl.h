@@ -340,7 +340,7 @@ int ulorl_token_loss_step_host(const ulorl_params_t* params,
  * synchronisation, device findings in the workspace status word, bit-identical results for equal inputs.  With
  *     a[t, v] = hidden[t] . W[v],  z = inv_temperature a,  p = softmax(z[t, :]),  lse = ln sum_v e^z
  * hidden [T,H], W [V,H] have the type `dtype`; the T x V logits are never written to global memory (CUDA-core
- * path: beyond one token panel of float32).  Any T >= 0; H a multiple of 8.
+ * path: beyond one token panel of float32).  Any T >= 0; H a multiple of 8; no size above 2^30.
  */
 typedef enum { ULORL_F16 = 2 } ulorl_logits_dtype_t;      /* further type of ulorl_logits_scores                   */
 
@@ -360,7 +360,7 @@ typedef struct {
   int32_t top_k;               /* scores: alternatives returned per token (0 .. ULORL_MAX_TOP, at most V);         */
                                /* distillation: entries per token of the teacher's list (1 .. ULORL_MAX_LIST)      */
   int32_t kernel_path;         /* AUTO, SIMT or TENSOR                                                             */
-  float inv_temperature;       /* kappa multiplying the logits; at most 1e6                                        */
+  float inv_temperature;       /* kappa multiplying the logits; 1e-6 .. 1e6                                        */
   int32_t bwd_panel_tokens;    /* backward: tokens per staging panel; 0 = library default                          */
   int32_t dw_accumulate;       /* backward: 0 overwrite d_W, 1 add into it                                         */
   int32_t dw_dtype;            /* ulorl_dtype_t of d_W                                                             */
@@ -371,7 +371,8 @@ typedef struct {
 
 /* Bytes of workspace of the calls below (pure host function; 0 on invalid params).  backward = 0: enough for
  * ulorl_token_scores and ulorl_distill_fwd; 1: for the backward calls as well.  Nothing in the workspace has to
- * survive from one call to the next; the status word is cleared by the forward calls, not by the backward ones. */
+ * survive from one call to the next; the status word is cleared by the forward calls, not by the backward ones (a
+ * workspace that only backward calls use starts with a zeroed one). */
 size_t ulorl_head_workspace_bytes(const ulorl_head_params_t* params, int32_t backward);
 
 /*
@@ -407,7 +408,7 @@ int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden
  * have probability zero; they come last among the alternatives, by rising id.  A row without any other entry has
  * lse = logp = top_logp = -inf and entropy 0.  A target outside [0, V) gets logp NaN (there is no workspace whose
  * status word could tell).  One kernel launch, no workspace; runs in [0, T) x [0, V) only, so padding columns may
- * hold anything.
+ * hold anything.  inv_temperature, T and V as above.
  */
 int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V, int64_t ld, int32_t top_k,
                         float inv_temperature, const int32_t* targets, float* logp, float* entropy, float* lse,

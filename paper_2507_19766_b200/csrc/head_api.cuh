@@ -29,6 +29,10 @@ struct HeadPlan {
 
 static bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 
+// A column that does not count stands at -1e30: times the scale that has to be far below every exponent, and finite.
+static bool scale_supported(float inv_temperature) { return inv_temperature >= 1e-6f && inv_temperature <= 1e6f; }
+constexpr int kHeadMaxSize = 1 << 30;              // sizes rounded up to a tile stay within int
+
 static int validate_head(const ulorl_head_params_t* p) {
   if (!p) return ULORL_ERR_INVALID_ARG;
   if (p->T < 0 || p->H <= 0 || p->V <= 0 || p->top_k < 0) return ULORL_ERR_INVALID_ARG;
@@ -38,7 +42,8 @@ static int validate_head(const ulorl_head_params_t* p) {
   if (p->kernel_path == ULORL_PATH_TENSOR_1CTA) return ULORL_ERR_UNSUPPORTED;
   if (p->kernel_path == ULORL_PATH_TENSOR && p->dtype != ULORL_BF16) return ULORL_ERR_UNSUPPORTED;
   if (!(p->inv_temperature > 0.f) || !std::isfinite(p->inv_temperature)) return ULORL_ERR_INVALID_ARG;
-  if (p->inv_temperature > 1e6f) return ULORL_ERR_UNSUPPORTED;      // exponents of absent columns have to stay finite
+  if (!scale_supported(p->inv_temperature)) return ULORL_ERR_UNSUPPORTED;
+  if (p->T > kHeadMaxSize || p->H > kHeadMaxSize || p->V > kHeadMaxSize) return ULORL_ERR_UNSUPPORTED;
   if (!(p->teacher_inv_temperature > 0.f) || !std::isfinite(p->teacher_inv_temperature)) return ULORL_ERR_INVALID_ARG;
   if (p->distill_mode < ULORL_DISTILL_RAW || p->distill_mode > ULORL_DISTILL_TAIL) return ULORL_ERR_INVALID_ARG;
   if (p->distill_mode != ULORL_DISTILL_RENORM && p->teacher_inv_temperature != 1.f) return ULORL_ERR_INVALID_ARG;
@@ -345,8 +350,7 @@ static int head_begin(const void* hidden, const void* W, void* workspace, size_t
 }
 
 // dz panels and the two gradient contractions.  row_p (and row_ins, targets) say what a row of dz is (flat: with beta = 0
-// in all of them); put_list
-// writes the teacher lists' columns of a panel, if there are any.
+// in all of them); put_list writes the teacher lists' columns of a panel, if there are any.
 static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W,
                         const int32_t* targets, const float4* row_p, const float* row_ins, bool flat,
                         const std::function<int(int, int)>& put_list, void* d_hidden, void* d_W_out, uint8_t* ws,
@@ -597,6 +601,7 @@ int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V,
   if (dtype != ULORL_F32 && dtype != ULORL_BF16 && dtype != ULORL_F16) return ULORL_ERR_UNSUPPORTED;
   if (top_k > ULORL_MAX_TOP) return ULORL_ERR_UNSUPPORTED;
   if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature)) return ULORL_ERR_INVALID_ARG;
+  if (!scale_supported(inv_temperature) || T > kHeadMaxSize || V > kHeadMaxSize) return ULORL_ERR_UNSUPPORTED;
   if (T == 0) return ULORL_OK;
   if ((top_k > 0) != (top_ids != nullptr) || (top_k > 0) != (top_logp != nullptr)) return ULORL_ERR_INVALID_ARG;
   if (logp && !targets) return ULORL_ERR_INVALID_ARG;

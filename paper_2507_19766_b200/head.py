@@ -21,9 +21,15 @@ import torch
 from .binding import BF16, F32, OK, CHeadParams, UlorlError, _PATH, load_library, status_string
 
 MAX_TOP, MAX_LIST = 32, 128
+_MAX_SIZE = 1 << 30
 _DISTILL = {"raw": 0, "renorm": 1, "tail": 2}
 _DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _LOGITS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: 2}
+
+
+def _check_sizes(*sizes: int) -> None:
+    if max(sizes) > _MAX_SIZE:
+        raise UlorlError(f"sizes beyond {_MAX_SIZE} are not supported")      # the C side takes 32 bits
 
 
 @dataclass
@@ -48,6 +54,7 @@ class HeadParams:
                                    ("kernel_path", self.kernel_path, _PATH), ("distill_mode", self.distill_mode, _DISTILL)):
             if value not in known:
                 raise UlorlError(f"{name}: {value!r} is not one of {sorted(known)}")
+        _check_sizes(self.T, self.H, self.V, self.top_k, self.bwd_panel_tokens)
         return CHeadParams(self.T, self.H, self.V, BF16 if self.dtype == "bf16" else F32, self.top_k,
                            _PATH[self.kernel_path], self.inv_temperature, self.bwd_panel_tokens, int(self.dw_accumulate),
                            BF16 if self.dw_dtype == "bf16" else F32, _DISTILL[self.distill_mode],
@@ -118,7 +125,9 @@ def alloc_head_workspace(p: HeadParams, device, backward: bool = True) -> torch.
     device = torch.device(device)
     with contextlib.nullcontext() if device.index is None else torch.cuda.device(device):
         # sizes go by the device's multiprocessor count
-        return torch.empty(head_workspace_bytes(p, backward), dtype=torch.uint8, device=device)
+        workspace = torch.empty(head_workspace_bytes(p, backward), dtype=torch.uint8, device=device)
+        workspace[:256].zero_()                              # the status word: backward calls only add to it
+        return workspace
 
 
 def _workspace(lib, cp: CHeadParams, workspace, hidden, device: int, backward: bool):

@@ -24,7 +24,8 @@ def test_struct_size_matches_header(lib):
 
 
 @pytest.mark.parametrize("kw", [dict(T=-1), dict(H=0), dict(V=0), dict(H=60), dict(top_k=-1), dict(top_k=129), dict(inv_temperature=0.0),
-                                dict(inv_temperature=float("nan")), dict(inv_temperature=float("inf")), dict(inv_temperature=2e6), dict(kernel_path="tensor_1cta"),
+                                dict(inv_temperature=float("nan")), dict(inv_temperature=float("inf")), dict(inv_temperature=2e6), dict(inv_temperature=5e-7),
+                                dict(T=2 ** 30 + 1), dict(V=2 ** 31 - 1), dict(T=2 ** 32 + 8), dict(kernel_path="tensor_1cta"),
                                 dict(dtype="f32", kernel_path="tensor"), dict(norm_tokens=-1), dict(bwd_panel_tokens=-1),
                                 dict(teacher_inv_temperature=0.5), dict(distill_mode="tail", teacher_inv_temperature=2.0),
                                 dict(distill_mode="renorm", teacher_inv_temperature=0.0)])
@@ -86,6 +87,7 @@ def test_logits_refusals(lib):
     f = lambda dtype=0, T=4, V=10, ld=10, k=2, kappa=1.0, logits=fake, targets=fake, ids=fake, logp=fake: lib.ulorl_logits_scores(
         logits, dtype, T, V, ld, k, kappa, targets, logp, None, None, ids, ids, None)
     assert f(dtype=3) == -2 and f(k=33, V=50, ld=50) == -2
+    assert f(kappa=2e6) == -2 and f(kappa=5e-7) == -2 and f(V=2 ** 31 - 1, ld=2 ** 31) == -2 and f(T=2 ** 30 + 1) == -2
     for kw in (dict(T=-1), dict(V=0), dict(ld=9), dict(k=-1), dict(k=11), dict(kappa=0.0), dict(kappa=float("nan")), dict(logits=None),
                dict(targets=None), dict(ids=None), dict(k=0), dict(logits=ctypes.c_void_p((1 << 20) + 2))):
         assert f(**kw) == -1, kw
@@ -100,3 +102,5 @@ def test_python_side_refusals(lib):
         U.logits_scores(torch.zeros(2, 5))
     with pytest.raises(U.UlorlError, match="CUDA"):
         U.distill_fwd(params(), h, w, None, None)
+    with pytest.raises(U.UlorlError, match="sizes"):                   # would be 8 in the 32 bits of the C side
+        U.HeadParams(T=2 ** 32 + 8, H=64, V=100).to_c()
