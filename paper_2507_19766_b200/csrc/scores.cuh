@@ -15,6 +15,7 @@
 
 #include "common.cuh"
 #include "simt.cuh"
+#include "umma_gemm.cuh"
 
 namespace ulorl {
 
@@ -153,7 +154,7 @@ struct RowState {
   float lane_max = NAN;                                             // no entry yet
 
   __device__ __forceinline__ bool plain() const { return m >= -1e29f && m <= 1e30f; }
-  __device__ __forceinline__ float one() const { return fmaf(delta, kLn2, 1.f); }     // 2^delta
+  __device__ __forceinline__ float one() const { return residue_ex2(delta); }
 
   // folds in n entries: cmax is the largest of them, x their values, not below kFloor; `any`: the lane has some.  All lanes
   // of a warp together.  `exact` gives entry j as it is.
@@ -165,10 +166,10 @@ struct RowState {
     const float wmax = __int_as_float(wi ^ ((wi >> 31) & 0x7FFFFFFF));
     const bool risen = wmax > m;                                    // the same in all lanes
     if (risen) {
-      const float ref_new = fminf(fmaxf(c2 * wmax, -1e35f), 1e35f);
+      const float ref_new = fminf(fmaxf(c2 * wmax, -1e37f), 1e37f);
       if (m > -INFINITY) {
         const float d = fmaxf(ref - ref_new, -1000.f), sc = fast_ex2(d), mine = own * one();
-        u = sc * (fmaf(d, s + mine, u) + own * delta);
+        u = sc * (fmaf(d, s + mine, u) + mine * delta);
         s = (s + mine) * sc;
         own = 0.f;
       }
@@ -191,6 +192,7 @@ struct RowState {
         if (equal > 0.f) {
           own = 1.f;
           ls = (equal - 1.f) * one();
+          lu = ls * delta;
         }
       }
       constexpr int kChains = n >= 8 ? 4 : 1;
@@ -392,7 +394,7 @@ logits_rows_kernel(const RowsArgs args) {
 
   // ---- merge lanes, then warps
   {
-    const float f = fmaf(-st.delta, kLn2, 1.f);                     // back from ref to c2 m: 2^-delta
+    const float f = residue_ex2(-st.delta);                         // back from ref to c2 m
     float s = st.s * f, u = fmaf(-st.delta, st.s, st.u) * f, n = st.own;
     if (abort_flag) s = __uint_as_float(0x7FC00000u);               // a copy that never came: the row's results are NaN
 #pragma unroll

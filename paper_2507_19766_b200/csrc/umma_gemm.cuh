@@ -338,24 +338,30 @@ __device__ __forceinline__ void put_bf16(uint32_t (&packed)[32], int idx, uint32
 // and, unlike that of -inf, so is the product with its exponent.
 constexpr float kNoColumn = -1e30f;
 
+// 2^d for the residue d of a rounded exponent: next to one in float32 unless the scaled logits are in the ten thousands.
+__device__ __forceinline__ float residue_ex2(float d) {
+  return fabsf(d) < 4.8828125e-4f ? fmaf(d, 0.6931471805599453f, 1.f) : ex2f(d);     // d^2 ln(2)^2 / 2 < 2^-24
+}
+
 // Running statistics of a row: m the maximum of the raw accumulators, r = sum 2^(c2 a - ref) over all entries but ONE
 // that equals m, u = sum 2^(c2 a - ref) (c2 a - ref).  Leaving the maximum's own 1 out keeps the relative precision of
 // 1 - p and of the entropy in sharply peaked rows, where r is 10^-6 and would lose most of its digits beside a one.
 // ref is c2 m rounded, so that an exponent is one fused multiply-add; delta is what the rounding took off, and
 // finish() puts it back.
 struct RestSums {
-  float m = -INFINITY, ref = 0.f, delta = 0.f, r = 0.f, u = 0.f;
+  float m = kNoColumn, ref = 0.f, delta = 0.f, r = 0.f, u = 0.f;
 
-  // `raw` holds 32 numbers (kNoColumn among them), cmax their maximum
+  // `raw` holds 32 numbers (kNoColumn among them), cmax their maximum.  A chunk of nothing but kNoColumn leaves m and ref
+  // as they are: a reference of c2 kNoColumn would be off by its rounding, 10^22
   template <bool kEnt>
   __device__ __forceinline__ void fold(const uint32_t (&raw)[32], float cmax, float c2) {
     const bool risen = cmax > m;
     if (risen) {                                       // a few times per row: harmonic in the number of chunks
       const float ref_new = c2 * cmax;
-      if (m > -INFINITY) {
+      if (m > kNoColumn) {
         const float d = fmaxf(ref - ref_new, -1000.f), sc = ex2f(d);
-        const float one = fmaf(delta, 0.6931471805599453f, 1.f);
-        if (kEnt) u = sc * (fmaf(d, r + one, u) + delta);
+        const float one = residue_ex2(delta);
+        if (kEnt) u = sc * (fmaf(d, r + one, u) + one * delta);
         r = (r + one) * sc;
       }
       m = cmax;
@@ -379,7 +385,7 @@ struct RestSums {
     if (risen) {
       // The new maximum's own 1 is in the sum.  Where the others are at least a quarter of it, taking it off costs
       // two of the chunk's 24 bits; where they are less the row may be a peaked one, and they are added without it.
-      sum -= fmaf(delta, 0.6931471805599453f, 1.f);
+      sum -= residue_ex2(delta);
       if (sum < 0.25f) {
         sum = -1.f;                                    // of the entries equal to m one does not count
 #pragma unroll
@@ -387,6 +393,7 @@ struct RestSums {
           const float a = __uint_as_float(raw[j]);
           sum += a == m ? 1.f : 0.f;
         }
+        sum *= residue_ex2(delta);
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           const float a = __uint_as_float(raw[j]);
@@ -397,13 +404,13 @@ struct RestSums {
     r += sum;
     if (kEnt) {
       v[0] = add2(add2(v[0], v[1]), add2(v[2], v[3]));
-      u += (v[0].x + v[0].y) - (risen ? delta : 0.f);
+      u += (v[0].x + v[0].y) - (risen ? residue_ex2(delta) * delta : 0.f);
     }
   }
   // (m, r, u) relative to c2 m itself; a row of nothing but columns that do not count is (-inf, 0, 0)
-  __device__ __forceinline__ float4 finish(bool any) const {
-    if (!any) return make_float4(-INFINITY, r != r ? r : 0.f, 0.f, 0.f);
-    const float f = fmaf(-delta, 0.6931471805599453f, 1.f);
+  __device__ __forceinline__ float4 finish() const {
+    if (!(m > kNoColumn)) return make_float4(-INFINITY, r != r ? r : 0.f, 0.f, 0.f);
+    const float f = residue_ex2(-delta);
     return make_float4(m, r * f, fmaf(-delta, r, u) * f, 0.f);
   }
 };
@@ -550,7 +557,6 @@ __device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int
     const bool row_ok = row < args.M;
     const int grow = args.row0 + row;
     RestSums sums;
-    bool any = false;
     int y = -1;
     if (Tr::scores && row_ok && args.targets != nullptr) {
       y = args.targets[grow];
@@ -646,7 +652,6 @@ __device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int
 #pragma unroll
         for (int g = 0; g < 4; ++g) gmax[g] = max_of_group(raw, g);
         const float cmax = fmaxf(fmaxf(gmax[0], gmax[1]), fmaxf(gmax[2], gmax[3]));
-        if (kMode == kModeDistill) any = any || cmax > kNoColumn;
         sums.fold<kEnt>(raw, cmax, c2);
         if constexpr (Tr::top > 0) {
           list.fold(raw, gmax, cmax, col0, n_tile > n_begin);
@@ -671,7 +676,7 @@ __device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int
           if (j < args.top_k) { args.top_val[at * args.top_k + j] = list.val[j]; args.top_id[at * args.top_k + j] = list.id[j]; }
       }
     }
-    if (row_ok) args.partials[at] = sums.finish(kMode == kModeDistill ? any : sums.m > -INFINITY);
+    if (row_ok) args.partials[at] = sums.finish();
   }
 }
 
@@ -999,6 +1004,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if (rp.z != 0.f) k_row = log2f(fabsf(rp.z)) - fmaf(rp.x, c2, rp.y);
         sign_mask = rp.z < 0.f ? 0x80008000u : 0u;
       }
+      // beta = 0: alpha goes into the exponent, c2 a + k_row, as long as what rounding takes off k_row (2^-24 of it) is
+      // little beside the rounding of dz to bf16
+      [[maybe_unused]] bool flat = false;
+      if (kMode == kModeDzRow) flat = args.row_flat && !__any_sync(0xffffffffu, fabsf(rp.x * c2) > 8192.f);
       if (kMode == kModeDz) {
         if (row_ok) {
           const float gl = args.grad_loss ? *args.grad_loss : 1.f;
@@ -1042,7 +1051,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
               if (nv1 >= 32) dz_chunk<true>(raw1, 32, c2, k_row, sign_mask, packed + 16);
               else dz_chunk<false>(raw1, nv1, c2, k_row, sign_mask, packed + 16);
             } else if (kMode == kModeDzRow) {
-              if (args.row_flat) {                             // beta = 0 everywhere: alpha goes into the exponent
+              if (flat) {
                 if (nv0 >= 32) dz_chunk<true>(raw0, 32, c2, k_row, sign_mask, packed);
                 else dz_chunk<false>(raw0, nv0, c2, k_row, sign_mask, packed);
                 if (nv1 >= 32) dz_chunk<true>(raw1, 32, c2, k_row, sign_mask, packed + 16);

@@ -126,3 +126,21 @@ def check_grads(d_hidden, d_W, dz, size, hidden, W, E, tensor_path, dw_dtype, d_
     if d_W_before is not None:
         want = want + d_W_before.double().cpu()
     close(d_W, want, slack, ("d_W", d_W.dtype))
+
+
+def check_low_temperature(out, z, targets, k):
+    """Scores of exact logits at a large scale, where only lse may round like the logits themselves.  A difference to the
+    maximum is exact but for the scale's rounding and its own (2^-23 relative); sums of positive terms and their
+    logarithm add 2^-20."""
+    ref = scores64(z, targets, k)
+
+    def close(got, want, what):
+        err = (got.double() - want).abs()
+        assert bool((err <= 2.0 ** -19 + 2.0 ** -21 * want.abs()).all()), (what, float(err.max()))
+    close(out.logp, ref["logp"], "logp")
+    close(out.top_logp, ref["top_logp"], "top_logp")
+    spread = (ref["logp_all"].exp() * (ref["logp_all"] + ref["entropy"][:, None]).abs()).sum(1)
+    err = (out.entropy.double() - ref["entropy"]).abs()
+    assert bool((err <= (2.0 ** -19 + 2.0 ** -21 * ref["entropy"]) * (2 + spread)).all()), ("entropy", float(err.max()))
+    assert torch.equal(out.top_ids.cpu(), ref["top_ids"].cpu())
+    assert bool(((out.lse.double() - ref["lse"]).abs() <= 2.0 ** -23 * ref["lse"].abs()).all())

@@ -312,6 +312,20 @@ def test_distillation_against_differences(mode):
     assert abs(got - slope) <= 1e-5 * size
 
 
+@pytest.mark.parametrize("kappa", [0.35, 0.7, 1.0, 1.1, 1.9])
+def test_lists_of_whole_chunks(kappa):
+    """Lists that hold every column of the first chunks of a sweep, of its last one, or of the vocabulary."""
+    for V, K, first in ((600, 64, 0), (257, 33, 224), (96, 96, 0)):
+        T = 70
+        hidden, W, _ = operands(T, 64, V, "bf16", seed=V)
+        g = torch.Generator().manual_seed(K)
+        ids = torch.stack([first + torch.randperm(K, generator=g) for _ in range(T)]).to(torch.int32).to(DEV)
+        logp = (torch.log_softmax(torch.randn(T, K, generator=g), 1) - 0.1).to(DEV)
+        mode = "raw" if K == V else "tail"
+        p = U.HeadParams(T=T, H=64, V=V, top_k=K, distill_mode=mode, inv_temperature=kappa)
+        check_distill(p, hidden, W, ids, logp, None, True)
+
+
 def test_overconfident_student_keeps_the_remainder():
     """Mode tail, a student that gives the list all but 10^-7: the remainder's log-prob is not a difference of ones."""
     T, H, V, K = 6, 64, 2048, 4
@@ -438,6 +452,72 @@ def test_captured_step_on_a_side_stream(dtype):
             for got in outs:
                 assert all(torch.equal(a, b) for a, b in zip(got, want[n]))
     del graphs
+
+
+@pytest.mark.parametrize("T,dtype", [(20, "bf16"), (300, "bf16"), (300, "f32")])
+def test_low_temperature_keeps_its_digits(T, dtype):
+    """Exact logits of half a million, scaled, that differ by tenths: scores, alternatives and gradients."""
+    H, V, k, kappa = 64, 3001, 8, 2.0 ** 13
+    g = torch.Generator().manual_seed(61)
+    W = torch.zeros(V, H)
+    W[:, 0] = 40.0
+    W[:, 1:9] = torch.randint(0, 4, (V, 8), generator=g).float() * 2.0 ** -14
+    hidden = torch.zeros(T, H)
+    hidden[:, 0] = 1.0
+    hidden[torch.arange(T), 1 + torch.arange(T) % 8] = 1.0
+    h, w = hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV)
+    targets = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).to(DEV)
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, inv_temperature=kappa)
+    out = U.token_scores(p, h, w, targets)
+    z = R.logits64(h, w, kappa)
+    R.check_low_temperature(out, z, targets, k)
+    for d_logp, d_ent in ((torch.randn(T, generator=g).to(DEV), None), (None, torch.randn(T, generator=g).to(DEV))):
+        d_h, d_W = U.token_scores_bwd(p, h, w, targets, out, d_logp, d_ent)
+        dz, size = R.scores_dz64(z, targets, kappa, d_logp, d_ent)
+        # the entropy's dz carries the errors of log p and of the entropy, 2^-18 each beside terms of their size
+        R.check_grads(d_h, d_W, dz, size, h, w, torch.full((T,), 2.0 ** -18), dtype == "bf16", "f32")
+    # the student's own list: no loss, and lists that leave the maximum out keep the scale of the rest
+    ids = out.top_ids.clone()
+    d = U.distill_fwd(p, h, w, ids, torch.full((T, k), math.log(1.0 / (2 * k)), device=DEV))
+    ref = R.distill64(z, ids, torch.full((T, k), math.log(1.0 / (2 * k))), None, "raw", kappa)
+    err = (d.kl.double().cpu() - ref["kl"]).abs()
+    assert bool((err <= 2.0 ** -19 + 2.0 ** -20 * ref["kl"].abs()).all()), float(err.max())
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on two streams, each with its own workspace, give what they give alone."""
+    sets = []
+    for seed, (T, V, k) in ((71, (900, 9001, 20)), (72, (40, 30001, 8))):
+        p = U.HeadParams(T=T, H=256, V=V, top_k=k, distill_mode="tail")
+        sets.append((p, operands(T, 256, V, "bf16", seed), teacher_lists(T, V, k, seed), U.alloc_head_workspace(p, DEV), torch.cuda.Stream()))
+
+    def calls(p, ops, lists, ws):
+        s = U.token_scores(p, *ops, workspace=ws)
+        g = U.token_scores_bwd(p, *ops, s, s.logp, None, workspace=ws)
+        d = U.distill_fwd(p, *ops[:2], *lists, workspace=ws)
+        return [s.logp, s.entropy, s.top_ids, *g, d.loss, *U.distill_bwd(p, *ops[:2], lists[0], d, workspace=ws)]
+    want = [calls(*a[:4]) for a in sets]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for a in sets:
+            with torch.cuda.stream(a[4]):
+                got.append(calls(*a[:4]))
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert all(torch.equal(b, c) for b, c in zip(x, y))
+
+
+def test_status_of_a_workspace_for_backward_calls():
+    """A workspace that has seen no forward call reads as clean."""
+    T, H, V = 70, 64, 500
+    hidden, W, targets = operands(T, H, V, "bf16", seed=81)
+    p = U.HeadParams(T=T, H=H, V=V)
+    torch.full((U.head_workspace_bytes(p),), 255, dtype=torch.uint8, device=DEV)         # dirty bytes for the allocator to hand out
+    out = U.token_scores(p, hidden, W, targets)
+    ws = U.alloc_head_workspace(p, DEV)
+    U.token_scores_bwd(p, hidden, W, targets, out, out.logp, workspace=ws)
+    assert B.check_status(ws) == B.OK
 
 
 def test_results_do_not_depend_on_the_run():

@@ -144,3 +144,31 @@ def test_long_offsets():
     z = flat.as_strided((T, V), (ld, 1))
     z.copy_(torch.randn(T, V, device=DEV))
     check(z, torch.arange(T, dtype=torch.int32, device=DEV), 8)
+
+
+@pytest.mark.parametrize("kappa", [1e-6, 1e6])
+def test_extreme_temperatures(kappa):
+    """Masked entries have no probability at either end, and the row is uniform or greedy."""
+    V, k = 3001, 8
+    g = torch.Generator(device=DEV).manual_seed(11)
+    for dtype in TYPES:
+        z = torch.randn(4, V, generator=g, device=DEV).to(dtype)
+        z[:, ::3] = -math.inf
+        z[2] = -math.inf
+        z[2, 5] = 1.0
+        targets = torch.tensor([1, 3, 5, 4], dtype=torch.int32, device=DEV)
+        out = check(z, targets, k, kappa=kappa)
+        if kappa < 1:
+            assert abs(float(out.entropy[0]) - math.log(V - (V + 2) // 3)) <= 2.0 ** -19
+        assert float(out.entropy[2]) == 0.0 and float(out.logp[2]) == 0.0
+
+
+def test_low_temperature_keeps_its_digits():
+    """Scaled logits of 4 million that differ by tenths: what the scaled maximum loses to rounding is put back."""
+    V, k, kappa = 5001, 12, 1e5
+    g = torch.Generator().manual_seed(12)
+    for T in (1, 7, 400):
+        z = (40.0 + torch.randint(0, 12, (T, V), generator=g).double() * 2.0 ** -18).float().to(DEV)
+        targets = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).to(DEV)
+        out = U.logits_scores(z, targets, top_k=k, inv_temperature=kappa)
+        R.check_low_temperature(out, float(torch.tensor(kappa)) * z.double(), targets, k)
