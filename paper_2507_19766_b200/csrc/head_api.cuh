@@ -11,6 +11,8 @@ constexpr int kHeadMaxSplits = kMaxRowLists / 2;   // a split leaves two partial
 
 struct HeadPlan {
   bool tensor;
+  int planes;                              // tensor path: 1, or 3 for float32 operands (bf16 planes)
+  int width;                               // columns of a plane of hidden and of W (H with one plane)
   bool small;                              // tensor path, few tokens: the forward calls go through a panel of logits
   int sms, workers;                        // workers: CTA pairs
   int n_split, tiles_per_split;            // vocabulary splits of the forward sweep
@@ -22,9 +24,9 @@ struct HeadPlan {
   int dh_acc, dw_acc_tiles;                // accumulators per unit of the two gradient contractions
   int dh_parts, dh_part_blocks, dh_part_rows;
   // forward scratch
-  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_top_pub, off_sorted, off_slots, off_list_z, off_logits, fwd_total;
+  size_t off_status, off_partials, off_acc_y, off_top_val, off_top_id, off_top_pub, off_sorted, off_slots, off_list_z, off_logits, off_planes, fwd_total;
   // backward scratch, over the same bytes
-  size_t off_row_p, off_row_ins, off_panel, off_dw_acc, off_parts, bwd_total;
+  size_t off_row_p, off_row_ins, off_panel, off_dw_acc, off_parts, off_planes_bwd, bwd_total;
 };
 
 static bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
@@ -33,6 +35,9 @@ static bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7
 static bool scale_supported(float inv_temperature) { return inv_temperature >= 1e-6f && inv_temperature <= 1e6f; }
 constexpr int kHeadMaxSize = 1 << 30;              // sizes rounded up to a tile stay within int
 
+// float32 operands as three planes side by side: columns stay within int
+static bool split_possible(const ulorl_head_params_t* p) { return p->H <= kHeadMaxSize / 2 && p->V <= kHeadMaxSize / 2; }
+
 static int validate_head(const ulorl_head_params_t* p) {
   if (!p) return ULORL_ERR_INVALID_ARG;
   if (p->T < 0 || p->H <= 0 || p->V <= 0 || p->top_k < 0) return ULORL_ERR_INVALID_ARG;
@@ -40,7 +45,6 @@ static int validate_head(const ulorl_head_params_t* p) {
   if (p->dw_dtype != ULORL_F32 && p->dw_dtype != ULORL_BF16) return ULORL_ERR_INVALID_ARG;
   if (p->kernel_path < ULORL_PATH_AUTO || p->kernel_path > ULORL_PATH_TENSOR_1CTA) return ULORL_ERR_INVALID_ARG;
   if (p->kernel_path == ULORL_PATH_TENSOR_1CTA) return ULORL_ERR_UNSUPPORTED;
-  if (p->kernel_path == ULORL_PATH_TENSOR && p->dtype != ULORL_BF16) return ULORL_ERR_UNSUPPORTED;
   if (!(p->inv_temperature > 0.f) || !std::isfinite(p->inv_temperature)) return ULORL_ERR_INVALID_ARG;
   if (!scale_supported(p->inv_temperature)) return ULORL_ERR_UNSUPPORTED;
   if (p->T > kHeadMaxSize || p->H > kHeadMaxSize || p->V > kHeadMaxSize) return ULORL_ERR_UNSUPPORTED;
@@ -49,6 +53,7 @@ static int validate_head(const ulorl_head_params_t* p) {
   if (p->distill_mode != ULORL_DISTILL_RENORM && p->teacher_inv_temperature != 1.f) return ULORL_ERR_INVALID_ARG;
   if (p->norm_tokens < 0 || p->bwd_panel_tokens < 0) return ULORL_ERR_INVALID_ARG;
   if (p->dw_accumulate != 0 && p->dw_accumulate != 1) return ULORL_ERR_INVALID_ARG;
+  if (p->kernel_path == ULORL_PATH_TENSOR && p->dtype == ULORL_F32 && !split_possible(p)) return ULORL_ERR_UNSUPPORTED;
   if (p->top_k > ULORL_MAX_LIST) return ULORL_ERR_UNSUPPORTED;
   if (p->H % 8 != 0) return ULORL_ERR_UNSUPPORTED;
   return ULORL_OK;
@@ -62,13 +67,34 @@ static int sgemm_parts(const HeadPlan& pl, int M, int N, int K, int* k_part) {
   return (K + *k_part - 1) / *k_part;
 }
 
-static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
+// Whether float32 operands go through the tensor cores: six products of bf16 planes against CUDA-core multiply-adds.
+// Modelled microseconds of a forward call per 10^6 of V x H, and what the planes cost a small one (measured 39 us for 43 at
+// 512 tokens x 4096, H 256; 31 for 29 at 512 x 1000, H 128; 199 for 254 at 1 x 32768, H 1024; 209 for 881 at 512 tokens).
+static bool split_pays(const ulorl_head_params_t* p, bool backward) {
+  if (!split_possible(p)) return false;
+  const double vh = 1e-6 * (double)p->V * (double)p->H;
+  if (backward) return vh > 0.02;          // three contractions (1 token, H 64: 38 us for 55 at V 1000; H 8, V 100: 33 for 24)
+  const double simt = 6.9 * vh * ((p->T + 127) / 128);
+  const double tensor = (2.4 * ((p->T + 255) / 256) + 2.0) * vh + 17.0;
+  return simt > tensor;
+}
+
+// float32 operands: tokens of a panel by default; and tokens (vocabulary entries) that one accumulator of d_W (of d_hidden)
+// adds up, the sums of several being added in float32 afterwards.  The tensor core cuts off a sum's last bits, mostly one
+// way: an error that grows with the length (d_W of 1024 tokens 1.3e-6 off in one sum, 6.5e-7 in two).  Panels of 512
+// tokens would do for d_W, but leave d_hidden few units (2048 tokens x 32768, H 2048: 4.5 ms instead of 3.6).
+constexpr int kSplitPanel = 2048, kSplitTokens = 512, kSplitEntries = 2048;
+
+static HeadPlan make_head_plan(const ulorl_head_params_t* p, bool backward) {
   HeadPlan pl{};
-  pl.tensor = p->dtype == ULORL_BF16 && p->kernel_path != ULORL_PATH_SIMT;
+  pl.planes = p->dtype == ULORL_F32 ? 3 : 1;
+  pl.tensor = p->kernel_path == ULORL_PATH_TENSOR ||
+              (p->kernel_path != ULORL_PATH_SIMT && (p->dtype == ULORL_BF16 || split_pays(p, backward)));
+  pl.width = pl.planes == 3 ? (int)align_up((size_t)p->H, 2 * kBK) : p->H;
   pl.sms = device_sm_count();
   pl.workers = std::max(1, pl.sms / 2);
   const int T = p->T, V = p->V, H = p->H;
-  pl.small = pl.tensor && T <= kSmallMaxTokens;
+  pl.small = pl.tensor && pl.planes == 1 && T <= kSmallMaxTokens;
   const size_t T1 = (size_t)std::max(T, 1), K = (size_t)p->top_k;
   const int tile_m = 2 * kBM;
   const int m_tiles = std::max(1, (T + tile_m - 1) / tile_m);
@@ -84,9 +110,10 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
     // 30 splits: 4.47, 4.62 and 5.84 million cycles without alternatives, with 8 and with 32).  Without lists every further
     // split is still a pass over W more: 4.52 ms with 30 splits, 3.8 with 9, under the power cap.
     const int list = p->top_k <= 0 || p->top_k > kMaxTop ? 0 : (p->top_k <= 8 ? 8 : kMaxTop);
-    const double tile = std::max(8.0 * H, list == 0 ? 5300.0 : (list == 8 ? 6000.0 : 7000.0));
+    const double contraction = 8.0 * (pl.planes == 3 ? kProducts * pl.width : H);
+    const double tile = std::max(contraction, list == 0 ? 5300.0 : (list == 8 ? 6000.0 : 7000.0));
     const double fill = list == 0 ? 10000.0 : (list == 8 ? 12000.0 : 105000.0);
-    const size_t live_bytes = (size_t)pl.workers * (size_t)tile_m * (size_t)H * 2;
+    const size_t live_bytes = (size_t)pl.workers * (size_t)tile_m * (size_t)(pl.planes * pl.width) * 2;
     const int s_max = std::min(kHeadMaxSplits, n_tiles);
     const int s_min = std::max(1, std::min((int)((live_bytes + kStatsHiddenBudget - 1) / kStatsHiddenBudget), s_max));
     auto cost_of = [&](int s) {
@@ -104,16 +131,16 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   }
   pl.n_partial = pl.tensor && !pl.small ? 2 * pl.n_split : 1;
   // backward panels
-  int panel = p->bwd_panel_tokens > 0 ? p->bwd_panel_tokens : (pl.tensor ? pl.workers * tile_m : kDefaultPanelSimt);
+  int panel = p->bwd_panel_tokens > 0 ? p->bwd_panel_tokens : (!pl.tensor ? kDefaultPanelSimt : (pl.planes == 3 ? kSplitPanel : pl.workers * tile_m));
   if (!pl.tensor) panel = std::min(panel, 32768);                   // rows are a grid dimension there
   const int unit = pl.tensor ? tile_m : kSimtTile;
   panel = (int)std::min<long>((long)align_up((size_t)panel, (size_t)unit), (long)align_up(T1, (size_t)unit));
   pl.panel_tokens = panel;
   pl.n_panels = (int)((T1 + panel - 1) / panel);
-  pl.dz_ld = align_up((size_t)V, pl.tensor ? 64 : 4);
+  pl.dz_ld = align_up((size_t)V, pl.tensor ? (pl.planes == 3 ? 2 * kBK : 64) : 4);
   pl.logits_ld = align_up((size_t)V, 4);
   const bool want_bf16 = p->dw_dtype == ULORL_BF16;
-  pl.dw_direct = pl.tensor && want_bf16 && pl.n_panels == 1 && !p->dw_accumulate;
+  pl.dw_direct = pl.tensor && want_bf16 && pl.n_panels == 1 && !p->dw_accumulate && (pl.planes == 1 || T <= kSplitTokens);
   pl.dw_acc = want_bf16 && !pl.dw_direct;
   // d_hidden: few token tiles make few units (256 x 512 outputs each), so the vocabulary is cut into parts until
   // the units fill the GPU; the parts are float32 and added in order
@@ -131,7 +158,10 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
     const int k_blocks = (V + kBK * atoms - 1) / (kBK * atoms);
     const int units = ((panel + tile_m - 1) / tile_m) * ((H + pl.dh_acc * kBN - 1) / (pl.dh_acc * kBN));
     int parts = units >= pl.workers ? 1 : pl.workers / units;
-    parts = std::max(1, std::min(parts, k_blocks * atoms / 16));            // a part keeps at least 1024 vocabulary entries
+    // a part keeps at least 1024 vocabulary entries; six times the work and sums of limited length with float32 operands
+    if (pl.planes == 3) parts = std::max(std::min(parts, k_blocks * atoms / 2), (V + kSplitEntries - 1) / kSplitEntries);
+    else parts = std::max(1, std::min(parts, k_blocks * atoms / 16));
+    parts = std::max(1, std::min(parts, k_blocks));
     pl.dh_part_blocks = (k_blocks + parts - 1) / parts;
     pl.dh_parts = (k_blocks + pl.dh_part_blocks - 1) / pl.dh_part_blocks;
     pl.dh_part_rows = (int)align_up((size_t)panel, (size_t)tile_m);
@@ -152,12 +182,15 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
   off = align_up(std::max(lists, teacher), 1024);
   pl.off_logits = off;    // forward passes that go through a panel of logits
   pl.fwd_total = off;
+  pl.off_planes = off;
+  const size_t plane_bytes = pl.tensor && pl.planes == 3 ? align_up(sizeof(__nv_bfloat16) * 3 * (size_t)pl.width * (T1 + (size_t)V), 1024) : 0;
+  pl.fwd_total += plane_bytes;
   if (pl.small || !pl.tensor) pl.fwd_total = align_up(off + sizeof(float) * (size_t)std::min(panel, (int)T1) * pl.logits_ld, 1024);
   off = 256;
   pl.off_row_p = off;     off = align_up(off + sizeof(float4) * T1, 256);
   pl.off_row_ins = off;   off = align_up(off + sizeof(float) * T1, 1024);
   pl.off_panel = off;
-  off = align_up(off + (size_t)panel * pl.dz_ld * (pl.tensor ? 2 : 4), 1024);
+  off = align_up(off + (size_t)panel * pl.dz_ld * (pl.tensor ? 2 * (size_t)pl.planes : 4), 1024);
   if (pl.dw_acc) { pl.off_dw_acc = off; off = align_up(off + sizeof(float) * (size_t)V * (size_t)H, 1024); }
   if (!pl.tensor && p->dtype == ULORL_F32) {      // float32 contractions cut over k
     pl.off_parts = off;
@@ -168,7 +201,9 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p) {
     pl.off_parts = off;
     off = align_up(off + sizeof(float) * (size_t)pl.dh_parts * (size_t)pl.dh_part_rows * (size_t)H, 1024);
   }
-  pl.bwd_total = std::max(off, pl.fwd_total);
+  pl.off_planes_bwd = off;
+  off += plane_bytes;
+  pl.bwd_total = off;
   return pl;
 }
 
@@ -187,15 +222,37 @@ static int launch_grad(const HeadPlan& pl, int acc, const CUtensorMap& ma, const
                   : launch_umma_impl<kMode, 2, 1>(ma, mb, mc, a, pl.sms, stream);
 }
 
+// hidden and W as the tensor cores take them: themselves, or their planes, written here.
+struct HeadOperands {
+  const void *hidden, *W;
+  uint64_t ld;                             // columns of a row, all planes
+};
+static int prepare_operands(const ulorl_head_params_t* p, const HeadPlan& pl, const void* hidden, const void* W, void* planes,
+                            HeadOperands* o, cudaStream_t stream) {
+  *o = {hidden, W, (uint64_t)p->H};
+  if (pl.planes == 1) return ULORL_OK;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(planes);
+  const size_t rows = (size_t)p->T + (size_t)p->V, blocks = (rows * (size_t)(pl.width / 4) + 255) / 256;
+  split_planes_kernel<<<(unsigned)std::min(blocks, (size_t)pl.sms * 16), 256, 0, stream>>>(
+      static_cast<const float*>(hidden), (size_t)p->T, static_cast<const float*>(W), (size_t)p->V, p->H, pl.width, out);
+  *o = {out, out + (size_t)p->T * 3 * (size_t)pl.width, (uint64_t)(3 * pl.width)};
+  return check_launch();
+}
+
 // The forward sweep of hidden against W on the tensor cores; `a` carries the mode's own fields.
 static int run_sweep(const ulorl_head_params_t* p, const HeadPlan& pl, int mode, UmmaArgs a, const void* hidden,
                      const void* W, uint8_t* ws, cudaStream_t stream) {
+  HeadOperands o;
+  int st = prepare_operands(p, pl, hidden, W, ws + pl.off_planes, &o, stream);
+  if (st != ULORL_OK) return st;
   CUtensorMap map_a, map_b;
-  int st = make_map_bf16(&map_a, hidden, (uint64_t)p->T, (uint64_t)p->H, (uint64_t)p->H, kBK, kBM);
+  st = make_map_bf16(&map_a, o.hidden, (uint64_t)p->T, o.ld, o.ld, kBK, kBM);
   if (st != ULORL_OK) return st;
-  st = make_map_bf16(&map_b, W, (uint64_t)p->V, (uint64_t)p->H, (uint64_t)p->H, kBK, kBN / 2);
+  st = make_map_bf16(&map_b, o.W, (uint64_t)p->V, o.ld, o.ld, kBK, kBN / 2);
   if (st != ULORL_OK) return st;
-  a.M = p->T; a.N = p->V; a.K = p->H;
+  a.M = p->T; a.N = p->V; a.K = pl.width;
+  a.n_products = pl.planes == 3 ? (int)kProducts : 0;
+  a.a_plane = a.b_plane = pl.planes == 3 ? pl.width : 0;
   a.m_tiles = (p->T + 2 * kBM - 1) / (2 * kBM);
   a.n_tiles = (p->V + kBN - 1) / kBN;
   a.n_split = pl.n_split;
@@ -362,14 +419,20 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
   if (pl.tensor) {
     __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + pl.off_panel);
     const int tile_m = 2 * kBM;
+    const bool split = pl.planes == 3;
+    const int n_products = split ? (int)kProducts : 0, dz_plane = split ? (int)pl.dz_ld : 0, op_plane = split ? pl.width : 0;
+    const uint64_t dz_row = (uint64_t)pl.planes * pl.dz_ld;
+    HeadOperands o;
+    st = prepare_operands(p, pl, hidden, W, ws + pl.off_planes_bwd, &o, stream);
+    if (st != ULORL_OK) return st;
     CUtensorMap map_hidden_k, map_w_k, map_w_mn, map_hidden_mn, map_dw, map_parts;
-    st = make_map_bf16(&map_hidden_k, hidden, (uint64_t)T, (uint64_t)H, (uint64_t)H, kBK, kBM);
+    st = make_map_bf16(&map_hidden_k, o.hidden, (uint64_t)T, o.ld, o.ld, kBK, kBM);
     if (st != ULORL_OK) return st;
-    st = make_map_bf16(&map_w_k, W, (uint64_t)V, (uint64_t)H, (uint64_t)H, kBK, kBN / 2);
+    st = make_map_bf16(&map_w_k, o.W, (uint64_t)V, o.ld, o.ld, kBK, kBN / 2);
     if (st != ULORL_OK) return st;
-    st = make_map_bf16(&map_w_mn, W, (uint64_t)V, (uint64_t)H, (uint64_t)H, 64, kBK);
+    st = make_map_bf16(&map_w_mn, o.W, (uint64_t)V, o.ld, o.ld, 64, kBK);
     if (st != ULORL_OK) return st;
-    st = make_map_bf16(&map_hidden_mn, hidden, (uint64_t)T, (uint64_t)H, (uint64_t)H, 64, kBK);
+    st = make_map_bf16(&map_hidden_mn, o.hidden, (uint64_t)T, o.ld, o.ld, 64, kBK);
     if (st != ULORL_OK) return st;
     st = pl.dw_direct ? make_map_bf16(&map_dw, d_W_out, (uint64_t)V, (uint64_t)H, (uint64_t)H, 64, kBM)
                       : make_map(&map_dw, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, d_W, (uint64_t)V, (uint64_t)H, (uint64_t)H, 32, kBM);
@@ -383,14 +446,15 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
     for (int t0 = 0, panel = 0; t0 < T; t0 += pl.panel_tokens, ++panel) {
       const int rows = std::min(T - t0, pl.panel_tokens);
       CUtensorMap dz_out, dz_k, dz_mn;
-      st = make_map_bf16(&dz_out, dz, (uint64_t)pl.panel_tokens, (uint64_t)pl.dz_ld, (uint64_t)pl.dz_ld, 64, kBM);
+      st = make_map_bf16(&dz_out, dz, (uint64_t)pl.panel_tokens, dz_row, dz_row, 64, kBM);
       if (st != ULORL_OK) return st;
-      st = make_map_bf16(&dz_k, dz, (uint64_t)rows, (uint64_t)pl.dz_ld, (uint64_t)pl.dz_ld, kBK, kBM);
+      st = make_map_bf16(&dz_k, dz, (uint64_t)rows, dz_row, dz_row, kBK, kBM);
       if (st != ULORL_OK) return st;
-      st = make_map_bf16(&dz_mn, dz, (uint64_t)rows, (uint64_t)pl.dz_ld, (uint64_t)pl.dz_ld, 64, kBK);
+      st = make_map_bf16(&dz_mn, dz, (uint64_t)rows, dz_row, dz_row, 64, kBK);
       if (st != ULORL_OK) return st;
       UmmaArgs a{};
-      a.M = rows; a.N = V; a.K = H;
+      a.M = rows; a.N = V; a.K = pl.width;
+      a.n_products = n_products; a.a_plane = a.b_plane = op_plane; a.out_plane = dz_plane;
       a.m_tiles = (rows + tile_m - 1) / tile_m;
       a.n_tiles = (int)((pl.dz_ld + kBN - 1) / kBN);
       a.group_m = kRasterGroup;
@@ -402,7 +466,8 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       a.row_flat = flat ? 1 : 0;
       a.dz_cols = (int)pl.dz_ld;
       a.status = reinterpret_cast<int*>(ws + pl.off_status);
-      st = launch_pair<kModeDzRow>(pl, map_hidden_k, map_w_k, dz_out, a, stream);
+      st = split ? launch_pair<kModeDzRow3>(pl, map_hidden_k, map_w_k, dz_out, a, stream)
+                 : launch_pair<kModeDzRow>(pl, map_hidden_k, map_w_k, dz_out, a, stream);
       if (st != ULORL_OK) return st;
       if (put_list) {
         st = put_list(t0, rows);
@@ -411,20 +476,30 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       // d_hidden[t0 + m, h] = sum_v dz[m, v] W[v, h]
       UmmaArgs b{};
       b.M = rows; b.N = H; b.K = V;
+      b.n_products = n_products; b.a_plane = dz_plane; b.b_plane = op_plane;
       b.m_tiles = (rows + tile_m - 1) / tile_m;
       b.group_m = kGradRasterGroup;
       b.row0 = t0;
       b.out_ld = (size_t)H;
       b.status = a.status;
-      if (pl.dh_parts > 1) {
+      if (split && pl.dh_parts == 1) {                             // float32 leaves the contraction as it is
+        st = make_map(&map_parts, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, static_cast<float*>(d_hidden) + (size_t)t0 * H, (uint64_t)rows,
+                      (uint64_t)H, (uint64_t)H, 32, kBM);
+        if (st != ULORL_OK) return st;
+      }
+      if (split || pl.dh_parts > 1) {
         b.n_split = pl.dh_parts;
         b.part_blocks = pl.dh_part_blocks;
         b.part_rows = pl.dh_part_rows;
         st = launch_grad<kModeDHiddenPart>(pl, pl.dh_acc, dz_k, map_w_mn, map_parts, b, stream);
         if (st != ULORL_OK) return st;
-        const size_t n = (size_t)rows * (size_t)H;
-        sum_parts_kernel<<<(unsigned)((n / 8 + 255) / 256), 256, 0, stream>>>(
-            parts, pl.dh_parts, (size_t)pl.dh_part_rows * (size_t)H, n, static_cast<__nv_bfloat16*>(d_hidden) + (size_t)t0 * H);
+        const size_t n = (size_t)rows * (size_t)H, stride = (size_t)pl.dh_part_rows * (size_t)H;
+        if (split && pl.dh_parts > 1)
+          sgemm_parts_kernel<<<(unsigned)((n / 4 + 255) / 256), 256, 0, stream>>>(parts, pl.dh_parts, stride, n,
+                                                                                  static_cast<float*>(d_hidden) + (size_t)t0 * H, 0);
+        else if (!split)
+          sum_parts_kernel<<<(unsigned)((n / 8 + 255) / 256), 256, 0, stream>>>(
+              parts, pl.dh_parts, stride, n, static_cast<__nv_bfloat16*>(d_hidden) + (size_t)t0 * H);
         ULORL_LAUNCH_CHECK();
       } else {
         b.d_hidden = static_cast<__nv_bfloat16*>(d_hidden);
@@ -432,19 +507,24 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
         if (st != ULORL_OK) return st;
       }
       // d_W[v, h] (+)= sum_m dz[m, v] hidden[t0 + m, h]
-      UmmaArgs c{};
-      c.M = V; c.N = H; c.K = rows;
-      c.m_tiles = (V + tile_m - 1) / tile_m;
-      c.group_m = kGradRasterGroup;
-      c.b_k0 = t0;
-      c.d_W = d_W;
-      c.out_ld = (size_t)H;
-      c.dz_cols = H;
-      c.accumulate = (panel > 0 || acc_into) ? 1 : 0;
-      c.status = a.status;
-      st = pl.dw_direct ? launch_grad<kModeDWBf16>(pl, pl.dw_acc_tiles, dz_mn, map_hidden_mn, map_dw, c, stream)
-                        : launch_grad<kModeDW>(pl, pl.dw_acc_tiles, dz_mn, map_hidden_mn, map_dw, c, stream);
-      if (st != ULORL_OK) return st;
+      const int terms = split ? kSplitTokens : rows;
+      for (int m0 = 0; m0 < rows; m0 += terms) {
+        UmmaArgs c{};
+        c.M = V; c.N = H; c.K = std::min(terms, rows - m0);
+        c.n_products = n_products; c.a_plane = dz_plane; c.b_plane = op_plane;
+        c.m_tiles = (V + tile_m - 1) / tile_m;
+        c.group_m = kGradRasterGroup;
+        c.a_k0 = m0;
+        c.b_k0 = t0 + m0;
+        c.d_W = d_W;
+        c.out_ld = (size_t)H;
+        c.dz_cols = H;
+        c.accumulate = (panel > 0 || m0 > 0 || acc_into) ? 1 : 0;
+        c.status = a.status;
+        st = pl.dw_direct ? launch_grad<kModeDWBf16>(pl, pl.dw_acc_tiles, dz_mn, map_hidden_mn, map_dw, c, stream)
+                          : launch_grad<kModeDW>(pl, pl.dw_acc_tiles, dz_mn, map_hidden_mn, map_dw, c, stream);
+        if (st != ULORL_OK) return st;
+      }
     }
   } else {
     float* dz = reinterpret_cast<float*>(ws + pl.off_panel);
@@ -501,8 +581,8 @@ extern "C" {
 
 size_t ulorl_head_workspace_bytes(const ulorl_head_params_t* params, int32_t backward) {
   if (validate_head(params) != ULORL_OK) return 0;
-  const HeadPlan pl = make_head_plan(params);
-  return backward ? pl.bwd_total : pl.fwd_total;
+  const size_t fwd = make_head_plan(params, false).fwd_total;
+  return backward ? std::max(fwd, make_head_plan(params, true).bwd_total) : fwd;
 }
 
 int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, const void* W, const int32_t* targets,
@@ -519,7 +599,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
   if (logp && !targets) return ULORL_ERR_INVALID_ARG;
   if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const HeadPlan pl = make_head_plan(params);
+  const HeadPlan pl = make_head_plan(params, false);
   st = head_begin(hidden, W, workspace, workspace_bytes, pl.fwd_total, pl.tensor && !pl.small && k > 0 ? pl.off_partials : 256, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -581,7 +661,7 @@ int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden
   if (!norm || !d_hidden || !d_W || (!d_logp && !d_entropy)) return ULORL_ERR_INVALID_ARG;
   if ((d_logp && (!logp || !targets)) || (d_entropy && !entropy)) return ULORL_ERR_INVALID_ARG;
   if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
-  const HeadPlan pl = make_head_plan(params);
+  const HeadPlan pl = make_head_plan(params, true);
   st = head_begin(hidden, W, workspace, workspace_bytes, pl.bwd_total, 0, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -635,7 +715,7 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
   }
   if (!teacher_ids || !teacher_logp || !kl || !norm || !coef || !entry_grad) return ULORL_ERR_INVALID_ARG;
   if (!aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
-  const HeadPlan pl = make_head_plan(params);
+  const HeadPlan pl = make_head_plan(params, false);
   st = head_begin(hidden, W, workspace, workspace_bytes, pl.fwd_total, 256, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -699,7 +779,7 @@ int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, con
   if (T == 0) return empty_head_bwd(params, d_W, stream);
   if (!teacher_ids || !norm || !coef || !entry_grad || !d_hidden || !d_W) return ULORL_ERR_INVALID_ARG;
   if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
-  const HeadPlan pl = make_head_plan(params);
+  const HeadPlan pl = make_head_plan(params, true);
   st = head_begin(hidden, W, workspace, workspace_bytes, pl.bwd_total, 0, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -711,10 +791,10 @@ int ulorl_distill_bwd(const ulorl_head_params_t* params, const void* hidden, con
     const unsigned blocks = (unsigned)((n + 255) / 256);
     if (pl.tensor)
       distill_put_kernel<<<blocks, 256, 0, stream>>>(rows, t0, K, V, params->inv_temperature, grad_loss, teacher_ids, entry_grad,
-                                                     reinterpret_cast<__nv_bfloat16*>(ws + pl.off_panel), pl.dz_ld);
+                                                     reinterpret_cast<__nv_bfloat16*>(ws + pl.off_panel), pl.dz_ld, pl.planes);
     else
       distill_put_kernel<<<blocks, 256, 0, stream>>>(rows, t0, K, V, params->inv_temperature, grad_loss, teacher_ids, entry_grad,
-                                                     reinterpret_cast<float*>(ws + pl.off_panel), pl.dz_ld);
+                                                     reinterpret_cast<float*>(ws + pl.off_panel), pl.dz_ld, 1);
     return check_launch();
   };
   return run_head_bwd(params, pl, hidden, W, nullptr, row_p, nullptr, true, put_list, d_hidden, d_W, ws, stream);

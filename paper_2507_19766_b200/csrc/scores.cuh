@@ -1070,14 +1070,43 @@ __global__ void distill_params_kernel(int T, float kappa, const float2* __restri
 template <typename TDz>
 __global__ void distill_put_kernel(int rows, int t0, int K, int V, float kappa, const float* __restrict__ grad_loss,
                                    const int* __restrict__ ids, const float* __restrict__ entry_grad,
-                                   TDz* __restrict__ panel, size_t ld) {
+                                   TDz* __restrict__ panel, size_t ld, int planes) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= (size_t)rows * K) return;
   const size_t at = (size_t)t0 * K + i;
   const int id = ids[at];
   if (id < 0 || id >= V) return;
   const float gl = grad_loss ? *grad_loss : 1.f;
-  from_f32(panel[(i / K) * ld + id], kappa * gl * entry_grad[at]);
+  float x = kappa * gl * entry_grad[at];
+  TDz* row = panel + (i / K) * ld * planes;                         // planes of ld columns
+  for (int q = 0; q < planes; ++q) {
+    from_f32(row[(size_t)q * ld + id], x);
+    x -= row_value(row[(size_t)q * ld + id]);
+  }
+}
+
+// Rows of float32 (hidden's T, then W's V, of `cols` columns) as three bf16 planes side by side, x = h + m + l: each is the
+// value rounded, the next what that left, so that all 24 bits are kept; planes are `width` columns wide, zero beyond
+// `cols`.  Bound by memory: 10 bytes an entry.
+__global__ void split_planes_kernel(const float* __restrict__ hidden, size_t T, const float* __restrict__ W, size_t V, int cols,
+                                    int width, __nv_bfloat16* __restrict__ out) {
+  const size_t quads = (T + V) * (size_t)(width / 4);
+  for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < quads; i += (size_t)gridDim.x * blockDim.x) {
+    const size_t r = i / (width / 4);
+    const int c = (int)(i - r * (width / 4)) * 4;
+    const float* x = r < T ? hidden + r * cols : W + (r - T) * cols;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < cols) v = __ldg(reinterpret_cast<const float4*>(x + c));                 // cols is a multiple of 8
+    __nv_bfloat16* dst = out + r * 3 * (size_t)width + c;
+#pragma unroll
+    for (int plane = 0; plane < 3; ++plane) {
+      const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+      *reinterpret_cast<uint2*>(dst + (size_t)plane * width) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      v.x -= __low2float(a); v.y -= __high2float(a);
+      v.z -= __low2float(b); v.w -= __high2float(b);
+    }
+  }
 }
 
 // d_hidden of a panel from the parts over the vocabulary, added in the order of the parts.

@@ -16,6 +16,11 @@
 //   kModeDzRow   dz = softmax * (alpha + beta log2 softmax) with per-row alpha and beta, one column overwritten
 //   kModeDHiddenPart  d_hidden over a part of the vocabulary, float32 (few token tiles: the parts fill the GPU)
 //   kModeDWBf16  d_W rounded to bf16 in the epilogue (all tokens in one launch)
+//   kModeDzRow3  kModeDzRow with dz written as three bf16 planes
+//
+// Float32 operands of scoring and distillation come as three bf16 planes x = h + m + l (24 bits, see split_planes_kernel)
+// side by side in the rows of a matrix, and a contraction runs over six products of planes: what is left out, m l and
+// smaller, is 2^-24 of the whole.  hh comes last, so that the accumulator is small while the small products are added.
 //
 // One kernel template umma_kernel<mode, CTAs per MMA, accumulators per unit>, persistent, one CTA per
 // SM, 192 threads: one thread of warp 0 feeds a shared-memory ring with TMA tile loads (128-byte
@@ -63,13 +68,17 @@ constexpr uint32_t kOutStageBytes = kBM * 128;
 // logits kernels use two atoms a stage, so that eight MMAs are queued per barrier round trip there too.
 enum UmmaMode { kModeStats = 0, kModeDz = 1, kModeDHidden = 2, kModeDW = 3,
                 kModeScores = 4, kModeScoresTop8 = 5, kModeScoresTop32 = 6, kModeDistill = 7,
-                kModeDzRow = 8, kModeDHiddenPart = 9, kModeDWBf16 = 10 };
+                kModeDzRow = 8, kModeDHiddenPart = 9, kModeDWBf16 = 10, kModeDzRow3 = 11 };
+
+// Planes of A and of B in the six products (h 0, m 1, l 2), two bits each: l h, h l, m m, h m, m h, h h.
+constexpr uint32_t kProducts = 6, kProductA = 0x118, kProductB = 0x052;
 
 template <int kMode>
 struct ModeTraits {
   static constexpr bool scores = (kMode >= kModeScores && kMode <= kModeScoresTop32);
   static constexpr bool sweep = (kMode == kModeStats || scores || kMode == kModeDistill);   // units of vocabulary splits
-  static constexpr bool dz = (kMode == kModeDz || kMode == kModeDzRow);
+  static constexpr bool dz_row = (kMode == kModeDzRow || kMode == kModeDzRow3);
+  static constexpr bool dz = (kMode == kModeDz || dz_row);
   static constexpr bool dh = (kMode == kModeDHidden || kMode == kModeDHiddenPart);
   static constexpr bool dw = (kMode == kModeDW || kMode == kModeDWBf16);
   static constexpr bool out_bf16 = dz || kMode == kModeDWBf16;        // 64-column bf16 tiles through staging
@@ -78,9 +87,11 @@ struct ModeTraits {
   static constexpr bool a_mn = dw;
   static constexpr bool b_mn = dh || dw;
   static constexpr bool wide = scores || kMode == kModeDistill;       // eight epilogue warps
-  static constexpr bool two_groups = (kMode == kModeDzRow || kMode == kModeDWBf16);   // two groups of four, 64 columns in turn
+  static constexpr bool two_groups = (dz_row || kMode == kModeDWBf16);   // two groups of four, 64 columns in turn
   static constexpr int epi_warps = wide || two_groups ? 8 : 4;
   static constexpr int threads = 64 + 32 * epi_warps;
+  static constexpr int out_planes = kMode == kModeDzRow3 ? 3 : 1;
+  static constexpr bool may_split = wide || kMode == kModeDzRow3 || kMode == kModeDHiddenPart || dw;   // float32 operands
   static constexpr int timing_kind = sweep ? 0 : (dz ? 1 : (dh ? 2 : 3));
 };
 
@@ -144,6 +155,10 @@ struct UmmaArgs {
   const float4* row_p;      // (m, log2 s, alpha, beta): L = c2 (a - m) - log2 s, dz = 2^L (alpha + beta L)
   const float* row_ins;     // dz at column targets[t]; read when targets is not NULL
   int row_flat;             // beta is zero in every row
+  // float32 operands as planes: n_products is kProducts (else 0), plane q starts q * a_plane (b_plane, out_plane) columns
+  // into a row (0 with one plane); K counts one plane
+  int n_products;
+  int a_plane, b_plane, out_plane;
   // kModeDHiddenPart: part s covers the k-blocks [s * part_blocks, (s + 1) * part_blocks) and writes rows
   // [s * part_rows, ...) of the output map; n_split parts
   int part_blocks, part_rows;
@@ -291,6 +306,32 @@ __device__ __forceinline__ void dz_row_chunk(const uint32_t (&raw)[32], int nval
     if (!kFull && j + 1 >= nvalid) v.y = 0.f;
     __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
     packed[j >> 1] = live ? *reinterpret_cast<uint32_t*>(&h) : 0u;
+  }
+}
+
+// The same as float32, in place of the logits.
+__device__ __forceinline__ void dz_row_values(uint32_t (&raw)[32], int nvalid, float c2, const float4& rp, bool live) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const float L = fmaf(__uint_as_float(raw[j]) - rp.x, c2, -rp.y);
+    raw[j] = live && j < nvalid ? __float_as_uint(ex2f(L) * fmaf(rp.w, L, rp.z)) : 0u;
+  }
+}
+// raw[idx] = x for an index only known at run time (see drop_column)
+__device__ __forceinline__ void put_value(uint32_t (&raw)[32], int idx, float x) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, %3;\n\t}"
+                 : "+r"(raw[j]) : "r"(idx), "r"(j), "f"(x));
+}
+// packed = the values rounded to bf16, raw = what that took off them
+__device__ __forceinline__ void take_plane(uint32_t (&raw)[32], uint32_t* packed) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(raw[j]), __uint_as_float(raw[j + 1]));
+    packed[j >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+    raw[j] = __float_as_uint(__uint_as_float(raw[j]) - __low2float(h));
+    raw[j + 1] = __float_as_uint(__uint_as_float(raw[j + 1]) - __high2float(h));
   }
 }
 
@@ -777,6 +818,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                       : (kMode == kModeDHiddenPart) ? args.m_tiles * args.n_tiles * args.n_split
                                                     : args.m_tiles * args.n_tiles;
 
+  const int n_products = Tr::may_split && args.n_products > 1 ? args.n_products : 1;
+
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (every CTA)
     // One thread runs the whole loop: nothing in it needs the other lanes, and a warp-wide
@@ -802,8 +845,12 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const int a_row = args.a_mn0 + (m_tile * kCta + cta_rank) * kBM;
         for (int n_tile = n_begin; n_tile < n_end; ++n_tile) {
           const int b_row = args.b_mn0 + n_tile * kUnitN + cta_rank * kBNcta;   // + kBN per further accumulator
+          for (int product = 0; product < n_products; ++product)
           for (int kb = kb_begin; kb < kb_end; ++kb) {
             if (!mbar_wait_bounded(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_p, kWaitLimitCycles)) goto producer_drain;
+            // a plane is a shift along the rows of the matrix, which hold k (K-major) or the operand's own index
+            const int pa = Tr::may_split ? (int)((kProductA >> (2 * product)) & 3u) * args.a_plane : 0;
+            const int pb = Tr::may_split ? (int)((kProductB >> (2 * product)) & 3u) * args.b_plane : 0;
             const uint32_t full = full0 + stage * (uint32_t)sizeof(uint64_t);
             if (kPair) {
               // both CTAs' bytes are counted on the issuing CTA's barrier, which alone is armed
@@ -815,36 +862,37 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             for (int t = 0; t < kKA; ++t) {
               const uint32_t sa = smem_base + stage * kStageBytesCta + t * kAtomBytesCta;
               const uint32_t sb = sa + kABytes;
-              const int ka = args.a_k0 + (kb * kKA + t) * kBK, kbb = args.b_k0 + (kb * kKA + t) * kBK;
+              const int ka = args.a_k0 + (kb * kKA + t) * kBK + (kAmn ? 0 : pa), a_mn = a_row + (kAmn ? pa : 0);
+              const int kbb = args.b_k0 + (kb * kKA + t) * kBK + (kBmn ? 0 : pb), b_mn = b_row + (kBmn ? pb : 0);
               if (kPair) {
                 if (kAmn) {
 #pragma unroll
-                  for (int j = 0; j < kBM / 64; ++j) tma_load_2d_pair(sa + j * kChunkBytes, &map_a, full, a_row + j * 64, ka, pol_a);
+                  for (int j = 0; j < kBM / 64; ++j) tma_load_2d_pair(sa + j * kChunkBytes, &map_a, full, a_mn + j * 64, ka, pol_a);
                 } else {
-                  tma_load_2d_pair(sa, &map_a, full, ka, a_row, pol_a);
+                  tma_load_2d_pair(sa, &map_a, full, ka, a_mn, pol_a);
                 }
 #pragma unroll
                 for (int q = 0; q < kAcc; ++q) {
                   if (kBmn) {
 #pragma unroll
                     for (int j = 0; j < kBNcta / 64; ++j)
-                      tma_load_2d_pair(sb + q * kBBytesCta + j * kChunkBytes, &map_b, full, b_row + q * kBN + j * 64, kbb, pol_b);
+                      tma_load_2d_pair(sb + q * kBBytesCta + j * kChunkBytes, &map_b, full, b_mn + q * kBN + j * 64, kbb, pol_b);
                   } else {
-                    tma_load_2d_pair(sb + q * kBBytesCta, &map_b, full, kbb, b_row + q * kBN, pol_b);
+                    tma_load_2d_pair(sb + q * kBBytesCta, &map_b, full, kbb, b_mn + q * kBN, pol_b);
                   }
                 }
               } else {
                 if (kAmn) {
 #pragma unroll
-                  for (int j = 0; j < kBM / 64; ++j) tma_load_2d(sa + j * kChunkBytes, &map_a, full, a_row + j * 64, ka);
+                  for (int j = 0; j < kBM / 64; ++j) tma_load_2d(sa + j * kChunkBytes, &map_a, full, a_mn + j * 64, ka);
                 } else {
-                  tma_load_2d(sa, &map_a, full, ka, a_row);
+                  tma_load_2d(sa, &map_a, full, ka, a_mn);
                 }
                 if (kBmn) {
 #pragma unroll
-                  for (int j = 0; j < kBNcta / 64; ++j) tma_load_2d(sb + j * kChunkBytes, &map_b, full, b_row + j * 64, kbb);
+                  for (int j = 0; j < kBNcta / 64; ++j) tma_load_2d(sb + j * kChunkBytes, &map_b, full, b_mn + j * 64, kbb);
                 } else {
-                  tma_load_2d(sb, &map_b, full, kbb, b_row);
+                  tma_load_2d(sb, &map_b, full, kbb, b_mn);
                 }
               }
             }
@@ -908,7 +956,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           const uint32_t buf_phase = (acc_iter / kBufs) & 1u;
           if (!mbar_wait_bounded(smem_u32(&bar_tmem_empty[buf]), buf_phase ^ 1u, abort_p, kWaitLimitCycles)) goto mma_done;
           const uint32_t tmem_d = tmem_base + buf * kUnitN;
+          for (int product = 0; product < n_products; ++product)
           for (int kb = kb_begin; kb < kb_end; ++kb) {
+            const bool last = kb == kb_end - 1 && product == n_products - 1;
             if (!ready && !mbar_wait_bounded(smem_u32(&bar_full[stage]), phase, abort_p, kWaitLimitCycles)) goto mma_done;
             tc_fence_after_sync();
             const uint64_t da = da_base + stage * stage_step;
@@ -921,7 +971,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 for (int k = 0; k < kBK / kUmmaK; ++k) {
                   const uint64_t daq = da + t * atom_step + k * a_step;
                   const uint64_t dbq = db + t * atom_step + q * (uint64_t)(kBBytesCta >> 4) + k * b_step;
-                  const uint32_t acc = (kb > kb_begin || t > 0 || k > 0) ? 1u : 0u;
+                  const uint32_t acc = (product > 0 || kb > kb_begin || t > 0 || k > 0) ? 1u : 0u;
                   if (kPair) umma_bf16_pair(tmem_d + q * kBN, daq, dbq, idesc, acc);
                   else umma_bf16(tmem_d + q * kBN, daq, dbq, idesc, acc);
                 }
@@ -929,10 +979,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             }
             if (kPair) {
               umma_commit_pair(smem_u32(&bar_empty[stage]), 3);                        // frees the slot in both CTAs
-              if (kb == kb_end - 1) umma_commit_pair(smem_u32(&bar_tmem_full[buf]), 3);  // accumulator ready
+              if (last) umma_commit_pair(smem_u32(&bar_tmem_full[buf]), 3);  // accumulator ready
             } else {
               umma_commit(smem_u32(&bar_empty[stage]));
-              if (kb == kb_end - 1) umma_commit(smem_u32(&bar_tmem_full[buf]));
+              if (last) umma_commit(smem_u32(&bar_tmem_full[buf]));
             }
             if (++stage == kStagesT) { stage = 0; phase ^= 1u; }
             ready = mbar_try_wait(smem_u32(&bar_full[stage]), phase);
@@ -979,7 +1029,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       float run_m = -INFINITY, run_s = 0.f, run_u = 0.f;
       int y = -1;
       float coef = 0.f, lse2 = 0.f;
-      if (kMode == kModeStats || kMode == kModeDz || (kMode == kModeDzRow && args.targets != nullptr)) {
+      if (kMode == kModeStats || kMode == kModeDz || (Tr::dz_row && args.targets != nullptr)) {
         if (row_ok) {
           y = args.targets[grow];
           if (y < 0 || y >= args.N) {
@@ -992,9 +1042,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const float4 p = args.partials[(size_t)split * args.T_total + grow];
         run_m = p.x; run_s = p.y; run_u = p.z;
       }
-      [[maybe_unused]] float4 rp = make_float4(0.f, 0.f, 0.f, 0.f);   // kModeDzRow
+      [[maybe_unused]] float4 rp = make_float4(0.f, 0.f, 0.f, 0.f);   // kModeDzRow, kModeDzRow3
       [[maybe_unused]] float ins = 0.f;
-      if (kMode == kModeDzRow && row_ok) {
+      if (Tr::dz_row && row_ok) {
         rp = args.row_p[grow];
         if (args.targets != nullptr) ins = args.row_ins[grow];
       }
@@ -1071,6 +1121,12 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 const __nv_bfloat16 hv = __float2bfloat16_rn(ins);
                 put_bf16(packed, y - col0, (uint32_t)(*reinterpret_cast<const uint16_t*>(&hv)));
               }
+            } else if (kMode == kModeDzRow3) {                 // float32 values in place of the logits
+              const bool live = rp.z != 0.f || rp.w != 0.f;
+              dz_row_values(raw0, nv0, c2, rp, live);
+              dz_row_values(raw1, nv1, c2, rp, live);
+              if (row_ok && y >= col0 && y < col0 + 32) put_value(raw0, y - col0, ins);
+              if (row_ok && y >= col0 + 32 && y < col0 + 64) put_value(raw1, y - col0 - 32, ins);
             } else {                                           // kModeDWBf16
 #pragma unroll
               for (int j = 0; j < 32; j += 2) {
@@ -1086,6 +1142,12 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
               const float vy = coef * (1.f - ex2f(fmaf(ay, c2, -lse2)));
               const __nv_bfloat16 hv = __float2bfloat16_rn(vy);
               put_bf16(packed, idx, (uint32_t)(*reinterpret_cast<const uint16_t*>(&hv)));
+            }
+#pragma unroll 1
+            for (int plane = 0; plane < Tr::out_planes; ++plane) {
+            if (Tr::out_planes > 1) {                          // the next plane: the values rounded, and what that left
+              take_plane(raw0, packed);
+              take_plane(raw1, packed + 16);
             }
             const uint32_t out_buf =
                 smem_base + kStagesT * kStageBytesCta + (Tr::two_groups ? (uint32_t)group : (stage_iter++ & 1u)) * kOutStageBytes;
@@ -1108,8 +1170,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             else epilogue_bar_sync();
             if (issuer) {
               // rows past the panel's capacity (d_W: past the vocabulary) are clipped
-              if (Tr::dz || tile_row < args.M) tma_store_2d(&map_c, out_buf, col0, (Tr::dz ? 0 : args.row0) + tile_row);
+              if (Tr::dz || tile_row < args.M) tma_store_2d(&map_c, out_buf, col0 + plane * args.out_plane, (Tr::dz ? 0 : args.row0) + tile_row);
               bulk_commit_group();
+            }
             }
           }
         }

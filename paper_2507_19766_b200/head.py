@@ -27,11 +27,6 @@ _DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 _LOGITS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: 2}
 
 
-def _check_sizes(*sizes: int) -> None:
-    if max(sizes) > _MAX_SIZE:
-        raise UlorlError(f"sizes beyond {_MAX_SIZE} are not supported")      # the C side takes 32 bits
-
-
 @dataclass
 class HeadParams:
     """Mirror of ulorl_head_params_t.  top_k: alternatives that token_scores returns, or entries of a teacher's list."""
@@ -54,7 +49,8 @@ class HeadParams:
                                    ("kernel_path", self.kernel_path, _PATH), ("distill_mode", self.distill_mode, _DISTILL)):
             if value not in known:
                 raise UlorlError(f"{name}: {value!r} is not one of {sorted(known)}")
-        _check_sizes(self.T, self.H, self.V, self.top_k, self.bwd_panel_tokens)
+        if self.T > _MAX_SIZE or self.H > _MAX_SIZE or self.V > _MAX_SIZE or self.top_k > MAX_LIST or self.bwd_panel_tokens > _MAX_SIZE:
+            raise UlorlError(f"sizes beyond {_MAX_SIZE} (top_k {MAX_LIST}) are not supported")      # the C side takes 32 bits
         return CHeadParams(self.T, self.H, self.V, BF16 if self.dtype == "bf16" else F32, self.top_k,
                            _PATH[self.kernel_path], self.inv_temperature, self.bwd_panel_tokens, int(self.dw_accumulate),
                            BF16 if self.dw_dtype == "bf16" else F32, _DISTILL[self.distill_mode],
@@ -229,6 +225,8 @@ def logits_scores(logits: torch.Tensor, targets=None, top_k: int = 0, inv_temper
     ld, step = logits.stride()
     if T <= 1:
         ld = V
+    if T > _MAX_SIZE or V > _MAX_SIZE:
+        raise UlorlError(f"logits: sizes beyond {_MAX_SIZE} are not supported")
     if (V > 1 and step != 1) or ld < V:
         raise UlorlError("logits: a row must be contiguous and rows must not overlap")
     if _elsewhere(device):

@@ -64,7 +64,7 @@ SIZES = [(1, 64, 1000, 5), (16, 72, 20001, 3), (17, 128, 2500, 20), (33, 64, 400
 
 
 @pytest.mark.parametrize("T,H,V,k", SIZES)
-@pytest.mark.parametrize("dtype,path", [("bf16", "auto"), ("bf16", "simt"), ("f32", "auto")])
+@pytest.mark.parametrize("dtype,path", [("bf16", "auto"), ("bf16", "simt"), ("f32", "simt"), ("f32", "tensor")])
 @pytest.mark.parametrize("grid", [True, False])
 def test_token_scores(T, H, V, k, dtype, path, grid):
     kappa = 1.0 if grid else 0.85
@@ -88,7 +88,7 @@ def test_ties_go_to_the_lowest_id():
     hidden = torch.randint(-1, 2, (T, H), generator=g).float()
     hidden[0] = 0                                            # every logit equal
     W = torch.randint(-1, 2, (V, H), generator=g).float()
-    for dtype, path in (("bf16", "auto"), ("bf16", "simt"), ("f32", "auto")):
+    for dtype, path in (("bf16", "auto"), ("bf16", "simt"), ("f32", "simt"), ("f32", "tensor")):
         h, w = hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV)
         p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, kernel_path=path)
         out = U.token_scores(p, h, w)
@@ -107,7 +107,7 @@ def test_peaked_rows_keep_their_digits():
     hidden = torch.zeros(T, H)
     hidden[torch.arange(T), torch.arange(T)] = 1.0
     W[:64] *= torch.linspace(10, 24, 64).to(torch.bfloat16).float()[:, None]
-    for dtype, path in (("bf16", "auto"), ("f32", "auto")):
+    for dtype, path in (("bf16", "auto"), ("f32", "simt"), ("f32", "tensor")):
         h, w = hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV)
         targets = torch.arange(T, dtype=torch.int32, device=DEV)
         p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, kernel_path=path)
@@ -152,7 +152,8 @@ def test_nan_hidden_row_stays_in_its_row():
 
 # ------------------------------------------------------------------------------------------------ gradients of scores
 @pytest.mark.parametrize("T,H,V", [(1, 64, 1000), (2, 8, 5), (129, 136, 257), (300, 256, 4099), (1000, 520, 700)])
-@pytest.mark.parametrize("dtype,path,dw", [("bf16", "auto", "bf16"), ("bf16", "auto", "f32"), ("bf16", "simt", "f32"), ("f32", "auto", "f32")])
+@pytest.mark.parametrize("dtype,path,dw", [("bf16", "auto", "bf16"), ("bf16", "auto", "f32"), ("bf16", "simt", "f32"), ("f32", "simt", "f32"),
+                                           ("f32", "tensor", "f32"), ("f32", "tensor", "bf16")])
 @pytest.mark.parametrize("which", ["both", "logp", "entropy"])
 def test_token_scores_gradients(T, H, V, dtype, path, dw, which):
     kappa = 0.8
@@ -176,8 +177,9 @@ def test_token_scores_gradients(T, H, V, dtype, path, dw, which):
         assert not bool(d_h[2:4].any())
 
 
-@pytest.mark.parametrize("dtype,dw", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
-def test_gradients_by_panels_and_accumulated(dtype, dw):
+@pytest.mark.parametrize("dtype,dw,path", [("bf16", "f32", "auto"), ("bf16", "bf16", "auto"), ("f32", "f32", "simt"), ("f32", "f32", "tensor"),
+                                           ("f32", "bf16", "tensor")])
+def test_gradients_by_panels_and_accumulated(dtype, dw, path):
     """Several token panels, d_W added into, against one panel: the same sums."""
     T, H, V = 700, 64, 900
     hidden, W, targets = operands(T, H, V, dtype, seed=9)
@@ -186,7 +188,7 @@ def test_gradients_by_panels_and_accumulated(dtype, dw):
     before = torch.randn(V, H, generator=g).to(DEV).to(DT[dw])
     dz, size = R.scores_dz64(R.logits64(hidden, W, 1.0), targets, 1.0, d_logp, None)
     for kw in (dict(bwd_panel_tokens=256), dict(dw_accumulate=True), dict(bwd_panel_tokens=512, dw_accumulate=True)):
-        p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, dw_dtype=dw, **kw)
+        p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, dw_dtype=dw, kernel_path=path, **kw)
         out = U.token_scores(p, hidden, W, targets)
         d_W = before.clone() if kw.get("dw_accumulate") else torch.full((V, H), 7.0, device=DEV, dtype=DT[dw])
         d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d_logp, None, d_W=d_W)
@@ -194,13 +196,14 @@ def test_gradients_by_panels_and_accumulated(dtype, dw):
                       before if kw.get("dw_accumulate") else None)
 
 
-def test_score_gradients_against_differences():
+@pytest.mark.parametrize("path", ["simt", "tensor"])
+def test_score_gradients_against_differences(path):
     """float32 head: the loss moves along a direction of (hidden, W) as the gradients say."""
     T, H, V, kappa = 24, 32, 300, 0.9
     hidden, W, targets = operands(T, H, V, "f32", seed=21)
     g = torch.Generator().manual_seed(2)
     d_logp, d_ent = torch.randn(T, generator=g).to(DEV), torch.randn(T, generator=g).to(DEV)
-    p = U.HeadParams(T=T, H=H, V=V, dtype="f32", inv_temperature=kappa)
+    p = U.HeadParams(T=T, H=H, V=V, dtype="f32", inv_temperature=kappa, kernel_path=path)
     out = U.token_scores(p, hidden, W, targets)
     d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d_logp, d_ent)
 
@@ -255,7 +258,7 @@ DISTILL_SIZES = [(1, 64, 1000, 5), (20, 64, 3001, 7), (40, 136, 2000, 33), (64, 
 
 @pytest.mark.parametrize("T,H,V,K", DISTILL_SIZES)
 @pytest.mark.parametrize("mode", ["raw", "renorm", "tail"])
-@pytest.mark.parametrize("dtype,path,dw", [("bf16", "auto", "bf16"), ("bf16", "simt", "f32"), ("f32", "auto", "f32")])
+@pytest.mark.parametrize("dtype,path,dw", [("bf16", "auto", "bf16"), ("bf16", "simt", "f32"), ("f32", "simt", "f32"), ("f32", "tensor", "f32")])
 def test_distillation(T, H, V, K, mode, dtype, path, dw):
     hidden, W, _ = operands(T, H, V, dtype, seed=T + K)
     ids, teacher = teacher_lists(T, V, K, seed=V)
@@ -273,8 +276,8 @@ def test_distillation(T, H, V, K, mode, dtype, path, dw):
             assert float(out.kl[2]) == 0.0 and not bool(d_h[2].any())
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_ids_listed_twice_and_out_of_range(dtype):
+@pytest.mark.parametrize("dtype,path", [("bf16", "auto"), ("f32", "simt"), ("f32", "tensor")])
+def test_ids_listed_twice_and_out_of_range(dtype, path):
     T, H, V, K = 12, 64, 600, 8
     hidden, W, _ = operands(T, H, V, dtype, seed=77)
     ids, teacher = teacher_lists(T, V, K, seed=5, ragged=False)
@@ -282,12 +285,12 @@ def test_ids_listed_twice_and_out_of_range(dtype):
     ids[1, :] = 17
     ids[2, 2], ids[2, 6] = ids[2, 0], ids[2, 0]
     for mode in ("raw", "renorm", "tail"):
-        p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode=mode)
+        p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode=mode, kernel_path=path)
         *_, ws = check_distill(p, hidden, W, ids, teacher, None, dtype == "bf16", grad_loss=-2.5)
         assert B.check_status(ws) == B.OK
     bad = ids.clone()
     bad[5, 3], bad[6, 0] = V, -7
-    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode="raw", norm_tokens=100)
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode="raw", norm_tokens=100, kernel_path=path)
     ws = U.alloc_head_workspace(p, DEV)
     U.distill_fwd(p, hidden, W, bad, teacher, workspace=ws)
     assert B.check_status(ws) == -6
@@ -360,7 +363,7 @@ def test_student_that_leaves_nothing_off_the_list():
             assert bool(torch.isfinite(d_h).all()) and bool(torch.isfinite(d_W).all()) and bool(torch.isfinite(out.kl).all())
 
 
-@pytest.mark.parametrize("dtype,path", [("f32", "auto"), ("bf16", "simt")])
+@pytest.mark.parametrize("dtype,path", [("f32", "simt"), ("bf16", "simt")])
 def test_forward_by_panels(dtype, path):
     """The CUDA-core path's forward passes by panels of tokens: the same results as in one."""
     T, H, V, k = 700, 64, 900, 6
@@ -373,6 +376,33 @@ def test_forward_by_panels(dtype, path):
     for x, y in ((a, b), (c, d)):
         for name, v in vars(x).items():
             assert torch.equal(v, getattr(y, name)), name
+
+
+def test_float32_planes_keep_their_digits():
+    """float32 operands on the tensor cores: long contractions (several panels of tokens, several parts of the
+    vocabulary) against 64 bits, relative to the whole; bf16 operands would be 10^-3 off, two planes 10^-5."""
+    T, H, V, k = 2500, 264, 6001, 8
+    hidden, W, targets = operands(T, H, V, "f32", seed=91)
+    ids, teacher = teacher_lists(T, V, k, seed=92)
+    g = torch.Generator().manual_seed(93)
+    d_logp = torch.randn(T, generator=g).to(DEV)
+    z = R.logits64(hidden, W, 1.0)
+    dz, _ = R.scores_dz64(z, targets, 1.0, d_logp, None)
+    ref = R.scores64(z, targets, k)
+    p = U.HeadParams(T=T, H=H, V=V, dtype="f32", top_k=k, distill_mode="tail", kernel_path="tensor")
+    out = U.token_scores(p, hidden, W, targets)
+    d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d_logp, None)
+    # a sum of n terms in float32: n/2 additions, each rounded or cut off by at most 2^-23, mostly one way
+    far = lambda got, want: float((got.double() - want).norm() / want.norm())
+    assert far(out.logp, ref["logp"]) <= H * 2.0 ** -24 and far(out.lse, ref["lse"]) <= H * 2.0 ** -24
+    slack = 4 * H * 2.0 ** -24                     # p is off by the error of its logit, about |z| = 4 times that
+    assert far(d_h, dz @ W.double()) <= slack + 2048 * 2.0 ** -24 and far(d_W, dz.t() @ hidden.double()) <= slack + 2048 * 2.0 ** -24
+    q = U.HeadParams(**{**vars(p), "kernel_path": "simt"})
+    a, b = (U.distill_fwd(x, hidden, W, ids, teacher) for x in (p, q))
+    (ah, aw), (bh, bw) = U.distill_bwd(p, hidden, W, ids, a), U.distill_bwd(q, hidden, W, ids, b)
+    assert far(a.kl, b.kl.double()) <= H * 2.0 ** -23
+    assert far(ah, bh.double()) <= 2 * (slack + 2048 * 2.0 ** -24) and far(aw, bw.double()) <= 2 * (slack + 2048 * 2.0 ** -24)
+    print("f32 planes: logp %.1e d_h %.1e d_W %.1e" % (far(out.logp, ref["logp"]), far(d_h, dz @ W.double()), far(d_W, dz.t() @ hidden.double())))
 
 
 # ------------------------------------------------------------------------------------------------ together
@@ -454,8 +484,8 @@ def test_captured_step_on_a_side_stream(dtype):
     del graphs
 
 
-@pytest.mark.parametrize("T,dtype", [(20, "bf16"), (300, "bf16"), (300, "f32")])
-def test_low_temperature_keeps_its_digits(T, dtype):
+@pytest.mark.parametrize("T,dtype,path", [(20, "bf16", "auto"), (300, "bf16", "auto"), (300, "f32", "simt"), (300, "f32", "tensor")])
+def test_low_temperature_keeps_its_digits(T, dtype, path):
     """Exact logits of half a million, scaled, that differ by tenths: scores, alternatives and gradients."""
     H, V, k, kappa = 64, 3001, 8, 2.0 ** 13
     g = torch.Generator().manual_seed(61)
@@ -467,7 +497,7 @@ def test_low_temperature_keeps_its_digits(T, dtype):
     hidden[torch.arange(T), 1 + torch.arange(T) % 8] = 1.0
     h, w = hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV)
     targets = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).to(DEV)
-    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, inv_temperature=kappa)
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, inv_temperature=kappa, kernel_path=path)
     out = U.token_scores(p, h, w, targets)
     z = R.logits64(h, w, kappa)
     R.check_low_temperature(out, z, targets, k)

@@ -26,7 +26,7 @@ def test_struct_size_matches_header(lib):
 @pytest.mark.parametrize("kw", [dict(T=-1), dict(H=0), dict(V=0), dict(H=60), dict(top_k=-1), dict(top_k=129), dict(inv_temperature=0.0),
                                 dict(inv_temperature=float("nan")), dict(inv_temperature=float("inf")), dict(inv_temperature=2e6), dict(inv_temperature=5e-7),
                                 dict(T=2 ** 30 + 1), dict(V=2 ** 31 - 1), dict(T=2 ** 32 + 8), dict(kernel_path="tensor_1cta"),
-                                dict(dtype="f32", kernel_path="tensor"), dict(norm_tokens=-1), dict(bwd_panel_tokens=-1),
+                                dict(dtype="f32", kernel_path="tensor", H=2 ** 29 + 8), dict(norm_tokens=-1), dict(bwd_panel_tokens=-1),
                                 dict(teacher_inv_temperature=0.5), dict(distill_mode="tail", teacher_inv_temperature=2.0),
                                 dict(distill_mode="renorm", teacher_inv_temperature=0.0)])
 def test_invalid_parameters(lib, kw):
