@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const Me
   const int width = a.k <= 8 ? 8 : (a.k <= 16 ? 16 : 32), per = 32 / width;      // lists a round takes
   const int e = lane % width, l0 = lane / width;
   int n = 0;
-  constexpr int kAhead = 6;                                         // loads in flight: the rounds depend on each other only by n
+  constexpr int kAhead = 12;                                        // loads in flight: the rounds depend on each other only by n
   for (int l = 0; l < a.n_split; l += per * kAhead) {
     float x[kAhead];
 #pragma unroll
@@ -728,13 +728,16 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const Me
       const bool keep = key_x != 0u && key_x >= least;
       const uint32_t votes = __ballot_sync(0xffffffffu, keep);
       const int pos = n + __popc(votes & ((1u << lane) - 1u));
-      // the id is fetched for the few that stay; an unused place of a list is -inf with id -1 and sorts behind
-      if (keep && pos < kMergeCandidates) {
-        const int i = __ldg(id + (l + j * per + l0) * stride + e);
-        cand[pos] = i < 0 ? 0ull : pack_entry(key_x, i);
-      }
+      if (keep && pos < kMergeCandidates) cand[pos] = ((unsigned long long)key_x << 32) | (uint32_t)((l + j * per + l0) * 32 + e);
       n += __popc(votes);
     }
+  }
+  __syncwarp();
+  // the ids of the few that stay, together; an unused place of a list is -inf with id -1 and sorts behind
+  for (int c = lane; c < min(n, kMergeCandidates); c += 32) {
+    const uint32_t from = (uint32_t)cand[c];
+    const int i = __ldg(id + (from / 32) * stride + from % 32);
+    cand[c] = i < 0 ? 0ull : pack_entry((uint32_t)(cand[c] >> 32), i);
   }
   __syncwarp();
   auto put = [&](int at, unsigned long long entry) {
@@ -746,6 +749,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const Me
       if (c >= n) { put(c, 0ull); continue; }                       // fewer than k entries are numbers
       const unsigned long long mine = cand[c];
       int rank = 0;
+#pragma unroll 8
       for (int o = 0; o < n; ++o) rank += cand[o] > mine ? 1 : 0;
       if (mine == 0ull) rank = n + 1;                               // an unused place: written below
       if (rank < a.k) put(rank, mine);

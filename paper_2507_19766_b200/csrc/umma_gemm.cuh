@@ -608,12 +608,14 @@ __device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int
     }
     // What the row's lists have seen bounds its top from below: where each of n of them has q entries of x or more,
     // n q >= top_k, the row has top_k.  Every list publishes its q-th largest group maximum (as an ordered key, 0 for
-    // none) and takes the least of the n published ones, once per tile; in a unit's first tile the accumulators are read
+    // none) and takes the least of the n published ones, in a unit's tiles 0, 1, 2, 4, 8, ... (between them the bound moves
+    // little, and the words are a round trip to L2 away); in a unit's first tile the accumulators are read
     // once for their group maxima before they are read for their entries.  Lists of one row run side by side, so nearly
     // all entries that are only large for their own split stay out: with 18 lists of 8448 columns each and k = 32 a
-    // list sees about 20 instead of 210.  The keys only rise and an entry of the row's top is never below them,
+    // list sees about 20 instead of 210.  n is no more than k: the least of 8 maxima is a better bound than the least of 32
+    // (1537 tokens x 32768, H 1024, 20 lists of 8: 135 -> 123 us a call).  The keys only rise and an entry of the row's top is never below them,
     // so what the merge picks does not depend on when they are read.  (Few, long lists: q > kNoted, nothing published.)
-    [[maybe_unused]] const int n_pub = min(2 * args.n_split, 32), q_pub = (args.top_k + n_pub - 1) / n_pub;
+    [[maybe_unused]] const int n_pub = max(1, min(min(2 * args.n_split, 32), args.top_k)), q_pub = (args.top_k + n_pub - 1) / n_pub;
     if constexpr (Tr::top > 0) list.clear(row_ok);
     [[maybe_unused]] int pos = 0, next_id = INT_MAX;  // kModeDistill: the next id of the row's list in this sweep
     [[maybe_unused]] const int* ids = nullptr;
@@ -648,7 +650,7 @@ __device__ __forceinline__ void wide_sweep(const UmmaArgs& args, int worker, int
               for (int g = 0; g < 4; ++g) list.note(max_of_group(raw, g));
             }
           }
-          if (row_ok) {
+          if (row_ok && ((n_tile - n_begin) & (n_tile - n_begin - 1)) == 0) {
             uint32_t* pub = args.top_pub + grow;
             const bool mine = 2 * split + half < n_pub;
             if (mine) publish_key(pub + (size_t)(2 * split + half) * args.T_total, list.noted(q_pub - 1));
