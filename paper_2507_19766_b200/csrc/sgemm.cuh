@@ -1,10 +1,14 @@
-// Float32 contraction on CUDA cores for the scoring and distillation calls with float32 operands:
+// Float32 contraction on CUDA cores for the scoring and distillation calls with float32 operands that are too small for the
+// tensor cores' planes to pay, or ask for this path:
 //   C[m, n] (+)= sum_k A(m, k) B(k, n)
 // with either operand contiguous along k or along its own index.  Blocks of 256 threads compute 128 x 128 outputs,
 // 8 x 8 a thread in two-element multiply-adds, from 16-deep slices of both operands that are double-buffered in shared
 // memory ([k][index], so that a thread's eight values are two 128-bit loads); the next slice is in registers while
 // one is multiplied.  Few output tiles and a long k (d_hidden: 8 tiles over 4096 vocabulary entries at the test size)
 // are cut over k into parts that a second kernel adds in order.
+// 512 x 4096 outputs, k 256: 29 us, 37 TFLOP/s, half of what the float32 units can do: 128 tiles on 148 multiprocessors, and
+// two warps a scheduler hide neither the 16 slices' barriers nor the start.  128 x 64 tiles took 32 us, 512 threads 35,
+// scalar multiply-adds 33, values of the next k fetched ahead into registers 30.
 #pragma once
 
 #include "common.cuh"

@@ -7,6 +7,7 @@
 // eighth or less of the stream and nearly every byte that arrives is W.  Every SM takes the same number of
 // vocabulary rows (a multiple of 16; its last tile is loaded with a shorter box), which the 256-row tiles of the sweep
 // cannot give: 594 tiles on 74 CTA pairs are 9 rounds for 8.03 tiles.
+// Measured for one token: 104 us, 6.0 TB/s of W (93 % of the copy rate); the whole call 119 us, through the sweep 237.
 // The logits go to global memory -- 4 bytes a vocabulary entry and token beside the 2 H bytes of its row of W -- and
 // the row kernel does the rest.
 #pragma once
