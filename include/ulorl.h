@@ -341,7 +341,7 @@ int ulorl_token_loss_step_host(const ulorl_params_t* params,
  *     a[t, v] = hidden[t] . W[v],  z = inv_temperature a,  p = softmax(z[t, :]),  lse = ln sum_v e^z
  * hidden [T,H], W [V,H] have the type `dtype`; the T x V logits are never written to global memory (CUDA-core
  * path: beyond one token panel of float32).  Float32 operands run on CUDA cores (SIMT) or, split into three bf16 planes
- * that keep all 24 bits, on the tensor cores (TENSOR; finite operands, the planes are 6 bytes an entry of workspace);
+ * that keep all 24 bits, on the tensor cores (TENSOR; finite operands below 3.3e38, the planes are 6 bytes an entry of workspace);
  * AUTO takes the faster one by the sizes.  Any T >= 0; H a multiple of 8; no size above 2^30.
  */
 typedef enum { ULORL_F16 = 2 } ulorl_logits_dtype_t;      /* further type of ulorl_logits_scores                   */

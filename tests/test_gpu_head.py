@@ -378,6 +378,27 @@ def test_forward_by_panels(dtype, path):
             assert torch.equal(v, getattr(y, name)), name
 
 
+@pytest.mark.parametrize("T,V,H,path", [(20, 1000, 64, "simt"), (300, 20000, 256, "tensor")])
+def test_float32_path_goes_by_the_sizes(T, V, H, path):
+    """What AUTO takes for float32 operands is one of the two paths, bit for bit and with its workspace; a forward of one fits a backward of the other."""
+    hidden, W, targets = operands(T, H, V, "f32", seed=T)
+    outs = []
+    for way in ("auto", path):
+        p = U.HeadParams(T=T, H=H, V=V, dtype="f32", top_k=4, kernel_path=way)
+        assert way == path or U.head_workspace_bytes(p, False) == U.head_workspace_bytes(U.HeadParams(**{**vars(p), "kernel_path": path}), False)
+        outs.append(U.token_scores(p, hidden, W, targets))
+    for name, v in vars(outs[0]).items():
+        assert torch.equal(v, getattr(outs[1], name)), name
+    # a forward of one path and a backward of the other belong together
+    d = torch.randn(T, generator=torch.Generator().manual_seed(1)).to(DEV)
+    z = R.logits64(hidden, W, 1.0)
+    dz, size = R.scores_dz64(z, targets, 1.0, d, None)
+    for fwd, bwd in (("simt", "tensor"), ("tensor", "simt")):
+        a, b = (U.HeadParams(T=T, H=H, V=V, dtype="f32", kernel_path=x) for x in (fwd, bwd))
+        s = U.token_scores(a, hidden, W, targets)
+        R.check_grads(*U.token_scores_bwd(b, hidden, W, targets, s, d, None), dz, size, hidden, W, 2 * R.logit_error(hidden, W, 1.0), False, "f32")
+
+
 def test_float32_planes_keep_their_digits():
     """float32 operands on the tensor cores: long contractions (several panels of tokens, several parts of the
     vocabulary) against 64 bits, relative to the whole; bf16 operands would be 10^-3 off, two planes 10^-5."""
