@@ -1,0 +1,109 @@
+"""Edges of token scoring and distillation: teacher lists that hold more or all of the probability, NaN weights beside
+alternatives, rows whose gradients are zero, vocabularies of millions, the planes of float32 operands one by one."""
+import math
+
+import pytest
+import torch
+
+import paper_2507_19766_b200 as U
+from paper_2507_19766_b200 import binding as B
+from tests import head_reference as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+PATHS = [("bf16", "auto"), ("bf16", "simt"), ("f32", "simt"), ("f32", "tensor")]
+
+
+def operands(T, H, V, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    W, hidden = torch.randn(V, H, generator=g) / 8, torch.randn(T, H, generator=g)
+    targets = torch.randint(0, V, (T,), generator=g, dtype=torch.int32)
+    return hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV), targets.to(DEV)
+
+
+# ------------------------------------------------------------------------------------------------ teacher lists
+def tail_loss(z, ids, teacher, weights, N):
+    """Mode tail in 64 bits: (loss, kl [T]).  The remainder 1 - sum q is an event of its own where there is one and the
+    student has entries for it."""
+    kl = []
+    for t in range(z.shape[0]):
+        ok = ids[t] >= 0
+        i, l = ids[t][ok], teacher[t][ok]
+        logp = torch.log_softmax(z[t], 0)
+        q = l.exp()
+        k = (q * (l - logp[i])).sum()
+        off = torch.ones(z.shape[1], dtype=torch.bool)
+        off[i] = False
+        rest = 1.0 - q.sum()
+        if bool(off.any()) and float(rest) > 0:
+            k = k + rest * (rest.log() - torch.logsumexp(logp[off], 0))
+        kl.append(k)
+    kl = torch.stack(kl)
+    return (weights * kl).sum() / N, kl
+
+
+def check_tail(p, hidden, W, ids, teacher, weights, tensor_path):
+    """Loss and gradients against the loss above and its derivative by autograd."""
+    ws = U.alloc_head_workspace(p, DEV)
+    out = U.distill_fwd(p, hidden, W, ids, teacher, weights, workspace=ws)
+    d_h, d_W = U.distill_bwd(p, hidden, W, ids, out, workspace=ws)
+    assert B.check_status(ws) == B.OK
+    kappa = p.inv_temperature
+    z = R.logits64(hidden, W, kappa).cpu().requires_grad_(True)
+    i, l, w = ids.cpu().long(), teacher.cpu().double(), weights.cpu().double()
+    loss, kl = tail_loss(z, i, l, w, p.T)
+    (dz,) = torch.autograd.grad(loss, z)
+    Q = torch.where(i >= 0, l.exp(), torch.zeros_like(l)).sum(1)
+    mass = Q.clamp(min=1.0)                        # what the log-probs of a row are weighted with
+    E = R.logit_error(hidden, W, kappa).cpu()
+    tol = (2 * E + 2.0 ** -19 + 2.0 ** -22 * z.detach().abs().amax(1)) * mass
+    kl, loss = kl.detach(), loss.detach()
+    assert bool(((out.kl.double().cpu() - kl).abs() <= 2 * tol + 2.0 ** -23 * kl.abs()).all()), (out.kl.cpu() - kl).abs().max()
+    slack = float(((2 * tol + 2.0 ** -23 * kl.abs()) * w).sum() / p.T + 2.0 ** -23 * loss.abs())
+    assert abs(float(out.loss[0]) - float(loss)) <= slack
+    # the terms of dz: the list's mass times p, q on the list, the remainder's share of p off it
+    prob = torch.softmax(z.detach(), 1)
+    on = torch.zeros_like(prob).scatter_add_(1, i.clamp(min=0), (i >= 0).double()) > 0
+    q = torch.zeros_like(prob).scatter_add_(1, i.clamp(min=0), torch.where(i >= 0, l.exp(), torch.zeros_like(l)))
+    rest_p = torch.where(on, torch.zeros_like(prob), prob).sum(1)
+    share = torch.where(rest_p > 0, (1 - Q).clamp(min=0.0) / rest_p, torch.zeros_like(Q))
+    size = mass[:, None] * prob + torch.where(on, q, prob * share[:, None])
+    R.check_grads(d_h, d_W, kappa * dz, kappa * w[:, None] / p.T * size, hidden, W, E + 2.0 ** -20, tensor_path, p.dw_dtype)
+    return out, d_h, d_W
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("T,H,V,K", [(20, 64, 700, 6), (130, 64, 1200, 9)])
+def test_lists_above_one(dtype, path, T, H, V, K):
+    """Mode tail, lists whose probabilities add up to more than one (log-probs stored in few bits, or of no distribution):
+    nothing is left for the remainder, and the gradient is that of the loss."""
+    hidden, W, _ = operands(T, H, V, dtype, seed=T)
+    g = torch.Generator().manual_seed(K)
+    ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(T)]).to(torch.int32)
+    total = torch.tensor([0.8, 1.003, 1.05, 1.3, 2.5]).repeat(T)[:T]
+    teacher = torch.log_softmax(torch.randn(T, K, generator=g), 1) + total.log()[:, None]
+    weights = (torch.rand(T, generator=g) < 0.9).float()
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode="tail", kernel_path=path, inv_temperature=0.9)
+    check_tail(p, hidden, W, ids.to(DEV), teacher.to(DEV), weights.to(DEV), dtype == "bf16" and path != "simt")
+
+
+@pytest.mark.parametrize("path", ["simt", "tensor"])
+def test_lists_above_one_against_differences(path):
+    """The returned loss moves along a direction of (hidden, W) as its gradients say, sum q = 1.3."""
+    T, H, V, K = 24, 32, 300, 5
+    hidden, W, _ = operands(T, H, V, "f32", seed=3)
+    g = torch.Generator().manual_seed(4)
+    ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(T)])
+    teacher = torch.log_softmax(torch.randn(T, K, generator=g), 1) + math.log(1.3)
+    p = U.HeadParams(T=T, H=H, V=V, dtype="f32", top_k=K, distill_mode="tail", kernel_path=path)
+    dev_ids = ids.to(torch.int32).to(DEV)
+    out = U.distill_fwd(p, hidden, W, dev_ids, teacher.to(DEV))
+    d_h, d_W = (x.double().cpu() for x in U.distill_bwd(p, hidden, W, dev_ids, out))
+    h, w = hidden.double().cpu(), W.double().cpu()
+    dh, dw = torch.randn(T, H, generator=g).double(), torch.randn(V, H, generator=g).double() / 8
+    eps = 1e-5
+    loss = lambda s: float(tail_loss((h + s * dh) @ (w + s * dw).t(), ids, teacher.double(), torch.ones(T).double(), T)[0])
+    got, size = float((d_h * dh).sum() + (d_W * dw).sum()), float((d_h * dh).abs().sum() + (d_W * dw).abs().sum())
+    # float32 gradients (a few 10^-6 of the sum of magnitudes), the difference's own eps^2
+    assert abs(got - (loss(eps) - loss(-eps)) / (2 * eps)) <= 1e-5 * size
