@@ -350,7 +350,8 @@ typedef enum { ULORL_F16 = 2 } ulorl_logits_dtype_t;      /* further type of ulo
  *   RAW     q_k = e^l_k: part of the teacher's distribution; what is not listed is left out of the loss
  *   RENORM  q = softmax(teacher_inv_temperature l) over the list (l may be raw logits)
  *   TAIL    q_k = e^l_k, and the remainder 1 - sum q is one more event, set against the student's
- *           probability of everything that is not listed; a list that adds up to more than one has no remainder    */
+ *           probability of everything that is not listed; a list that adds up to more than one has no remainder,
+ *           nor has a list of the whole vocabulary (it counts as in RAW)                                            */
 typedef enum { ULORL_DISTILL_RAW = 0, ULORL_DISTILL_RENORM = 1, ULORL_DISTILL_TAIL = 2 } ulorl_distill_mode_t;
 
 #define ULORL_MAX_TOP 32      /* alternatives per token of the scoring calls                                       */
@@ -420,7 +421,8 @@ int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V,
  * Distillation from a teacher's top logits, top_k entries per token: teacher_ids [T][top_k] int32 in any order, -1 =
  * no entry; teacher_logp [T][top_k] f32; weights [T] f32 or NULL (= 1).  With q as the mode says, Q = sum_k q_k and
  * P the student's probability of the listed ids:
- *   kl_t = sum_k q_k (ln q_k - ln p[ids_k])  (+ (1 - Q)(ln(1 - Q) - ln(1 - P)) in mode TAIL with Q < 1; 0 for an empty list)
+ *   kl_t = sum_k q_k (ln q_k - ln p[ids_k])  (+ (1 - Q)(ln(1 - Q) - ln(1 - P)) in mode TAIL, where Q < 1 and some id is
+ *   not listed; 0 for an empty list)
  *   loss = 1/N sum_t weights_t kl_t
  * An id that is listed twice is two entries of one event: its probabilities add in the gradient.  An id outside
  * [-1, V) is reported in the status word and left out.  Outputs: loss[1], kl[T], lse[T] (optional), and for the

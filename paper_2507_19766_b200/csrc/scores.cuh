@@ -998,14 +998,16 @@ __device__ __forceinline__ void distill_row(const DistillRowArgs& a, int t) {
   Q = warp_sum(Q);
   kl = warp_sum(kl);
   // Off the list d kl / d z_j is Q p_j, in mode tail (Q + rest_q) p_j - rest_q p_j / rest_p, rest_q = max(1 - Q, 0): a list
-  // that adds up to more than one leaves no remainder, and its loss weighs log-probs of Q in all.  Both are kept as a
-  // multiple of p_j / rest_p, the softmax over what is not listed: for a student that leaves next to nothing there, p_j and
-  // rest_p underflow in float32, their quotient and the multiple do not.
+  // that adds up to more than one leaves no remainder, and its loss weighs log-probs of Q in all.  A list of every id has
+  // none either (m_off is -inf): what a softmax of float32 log-probs leaves to one, 10^-8 or so, would be set against a
+  // probability of zero, a loss of infinity.  Both are kept as a multiple of p_j / rest_p, the softmax over what is not
+  // listed: for a student that leaves next to nothing there, p_j and rest_p underflow in float32, their quotient and the
+  // multiple do not.
   const double rest_p = rest / (rest + on);
   double c_on = Q, c_off = Q * rest_p;
   if (a.mode == ULORL_DISTILL_TAIL) {
-    const double rest_q = fmax(1.0 - Q, 0.0);
-    c_on = Q > 1.0 ? Q : 1.0;                                      // Q + rest_q
+    const double rest_q = m_off > -INFINITY ? fmax(1.0 - Q, 0.0) : 0.0;
+    c_on = Q > 1.0 || m_off == -INFINITY ? Q : 1.0;                // Q + rest_q
     c_off = c_on * rest_p - rest_q;
     if (rest_q > 0.0) kl += rest_q * (log(rest_q) - ln_rest);
   }

@@ -107,3 +107,18 @@ def test_lists_above_one_against_differences(path):
     got, size = float((d_h * dh).sum() + (d_W * dw).sum()), float((d_h * dh).abs().sum() + (d_W * dw).abs().sum())
     # float32 gradients (a few 10^-6 of the sum of magnitudes), the difference's own eps^2
     assert abs(got - (loss(eps) - loss(-eps)) / (2 * eps)) <= 1e-5 * size
+
+
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("T,V", [(20, 40), (20, 128), (130, 96), (70, 1)])
+def test_lists_of_the_whole_vocabulary(dtype, path, T, V):
+    """Mode tail, lists that hold every id and add up to a little less than one (a softmax stored in float32), to a tenth less,
+    or to more: the student has no entry for a remainder, and the loss is that of the list."""
+    hidden, W, _ = operands(T, 64, V, dtype, seed=T + V)
+    g = torch.Generator().manual_seed(V)
+    ids = torch.stack([torch.randperm(V, generator=g) for _ in range(T)]).to(torch.int32).to(DEV)
+    total = torch.tensor([1 - 1e-6, 0.9, 1.1]).double().repeat(T)[:T]
+    teacher = (torch.log_softmax(torch.randn(T, V, generator=g).double(), 1) + total.log()[:, None]).float().to(DEV)
+    p = U.HeadParams(T=T, H=64, V=V, dtype=dtype, top_k=V, distill_mode="tail", kernel_path=path)
+    out, d_h, d_W = check_tail(p, hidden, W, ids, teacher, torch.ones(T, device=DEV), dtype == "bf16" and path != "simt")
+    assert bool(torch.isfinite(out.loss).all()) and bool(torch.isfinite(out.kl).all())
