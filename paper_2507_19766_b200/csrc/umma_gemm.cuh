@@ -492,8 +492,10 @@ struct TopList {
     val[0] = above[0] ? x : val[0];
     id[0] = above[0] ? i : id[0];
   }
-  // Notes a group's maximum for what the row's lists publish (see wide_sweep).
+  // Notes a group's maximum for what the row's lists publish (see wide_sweep).  A group of NaN has none: min and max both
+  // return the number beside a NaN, which would stand in `best` twice.
   __device__ __forceinline__ void note(float x) {
+    x = fmaxf(x, -INFINITY);
 #pragma unroll
     for (int j = 0; j < kNoted; ++j) {
       const float hi = fmaxf(best[j], x);

@@ -122,3 +122,22 @@ def test_lists_of_the_whole_vocabulary(dtype, path, T, V):
     p = U.HeadParams(T=T, H=64, V=V, dtype=dtype, top_k=V, distill_mode="tail", kernel_path=path)
     out, d_h, d_W = check_tail(p, hidden, W, ids, teacher, torch.ones(T, device=DEV), dtype == "bf16" and path != "simt")
     assert bool(torch.isfinite(out.loss).all()) and bool(torch.isfinite(out.kl).all())
+
+
+# ------------------------------------------------------------------------------------------------ alternatives
+def test_nan_columns_beside_alternatives():
+    """Eight adjacent NaN rows of W in every stretch of 128 columns, and one logit per stretch far above the others: the NaN
+    columns stand for no entry, so the alternatives are those of the path that looks at every logit."""
+    T, H, V, k = 70, 64, 2560, 32
+    g = torch.Generator().manual_seed(12)
+    hidden, W = torch.randint(1, 3, (T, H), generator=g).float(), torch.randint(-3, 4, (V, H), generator=g).float() / 8
+    W[5::128] = 2.0                                          # far above: 2 sum h, against noise of 0.25 sqrt(H) h
+    for first in range(120, V, 128):
+        W[first:first + 8] = float("nan")
+    for dtype in ("bf16", "f32"):
+        h, w = hidden.to(DT[dtype]).to(DEV), W.to(DT[dtype]).to(DEV)
+        ids = [U.token_scores(U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=k, kernel_path=path), h, w).top_ids.cpu()
+               for path in ("tensor", "simt")]
+        ref = R.scores64(R.logits64(h, w, 1.0), None, k)     # all sums are exact
+        assert torch.equal(ids[1], ref["top_ids"].cpu())
+        assert torch.equal(ids[0], ref["top_ids"].cpu())
