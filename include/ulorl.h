@@ -418,6 +418,15 @@ int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V,
                         int32_t* top_ids, float* top_logp, void* cuda_stream);
 
 /*
+ * Self-test of the failure path of ulorl_logits_scores' kernel (see ulorl_selftest_bounded_wait): float32 logits [T][V],
+ * 16-byte aligned, T 1 .. 65536, V at least 4096, whose copies to shared memory are never issued.  Every block's wait gives up
+ * after limit_cycles SM clocks (1e3 .. 1e8), sets the timeout bit in the workspace status word and returns normally: lse
+ * and top_logp are NaN, top_ids -1.
+ */
+int ulorl_selftest_logits_wait(const float* logits, int32_t T, int32_t V, int32_t top_k, float* lse, int32_t* top_ids,
+                               float* top_logp, void* workspace, int64_t limit_cycles, void* cuda_stream);
+
+/*
  * Distillation from a teacher's top logits, top_k entries per token: teacher_ids [T][top_k] int32 in any order, -1 =
  * no entry; teacher_logp [T][top_k] f32; weights [T] f32 or NULL (= 1).  With q as the mode says, Q = sum_k q_k and
  * P the student's probability of the listed ids:

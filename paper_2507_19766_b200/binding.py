@@ -77,7 +77,7 @@ EXPORTS = ("ulorl_workspace_bytes", "ulorl_token_loss_fwd", "ulorl_token_loss_de
            "ulorl_token_loss_decide_static", "ulorl_group_advantages", "ulorl_sequence_entropy_partials",
            "ulorl_sequence_entropy_combine", "ulorl_decision_thresholds", "ulorl_selftest_bounded_wait",
            "ulorl_head_workspace_bytes", "ulorl_token_scores", "ulorl_token_scores_bwd", "ulorl_logits_scores",
-           "ulorl_distill_fwd", "ulorl_distill_bwd")
+           "ulorl_distill_fwd", "ulorl_distill_bwd", "ulorl_selftest_logits_wait")
 STATIC_MAX_TOKENS, STATIC_MAX_SEQS = 1 << 20, 1 << 16
 KERNEL_KINDS = ("stats", "dz", "d_hidden", "d_W")
 
@@ -142,6 +142,8 @@ def load_library() -> ctypes.CDLL:
     lib.ulorl_logits_scores.restype = ctypes.c_int
     lib.ulorl_logits_scores.argtypes = ([vp] + [ctypes.c_int32] * 3 + [ctypes.c_int64, ctypes.c_int32, ctypes.c_float] +
                                         [vp] * 7)
+    lib.ulorl_selftest_logits_wait.restype = ctypes.c_int
+    lib.ulorl_selftest_logits_wait.argtypes = [vp] + [ctypes.c_int32] * 3 + [vp] * 4 + [ctypes.c_int64, vp]
     lib.ulorl_distill_fwd.restype = ctypes.c_int
     lib.ulorl_distill_fwd.argtypes = [hp] + [vp] * 11 + [vp, ctypes.c_size_t, vp]
     lib.ulorl_distill_bwd.restype = ctypes.c_int

@@ -354,7 +354,7 @@ static int logits_panel(const ulorl_head_params_t* p, const HeadPlan& pl, const 
 
 // Rows are spread over clusters until there are two blocks a multiprocessor, as long as a block keeps four loads a
 // thread; more than eight blocks a cluster have to be asked for, once per device.
-template <typename T>
+template <typename T, bool kHeld = false>
 static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   static bool opted_in[kMaxDevices] = {};
   int dev = 0;
@@ -362,8 +362,8 @@ static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   {
     std::lock_guard<std::mutex> lock(g_setup_mutex);
     if (!opted_in[dev]) {
-      if (cudaFuncSetAttribute(logits_rows_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-          cudaFuncSetAttribute(logits_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem) != cudaSuccess)
+      if (cudaFuncSetAttribute(logits_rows_kernel<T, kHeld>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+          cudaFuncSetAttribute(logits_rows_kernel<T, kHeld>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem) != cudaSuccess)
         return ULORL_ERR_CUDA;
       opted_in[dev] = true;
     }
@@ -383,7 +383,7 @@ static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, logits_rows_kernel<T>, a) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, logits_rows_kernel<T, kHeld>, a) != cudaSuccess) {
     (void)cudaGetLastError();
     return ULORL_ERR_CUDA;
   }
@@ -699,6 +699,23 @@ int ulorl_logits_scores(const void* logits, int32_t dtype, int32_t T, int32_t V,
                             : (dtype == ULORL_BF16 ? launch_rows<__nv_bfloat16>(a, sms, stream) : launch_rows<__half>(a, sms, stream));
 }
 
+int ulorl_selftest_logits_wait(const float* logits, int32_t T, int32_t V, int32_t top_k, float* lse, int32_t* top_ids, float* top_logp,
+                               void* workspace, int64_t limit_cycles, void* cuda_stream) {
+  if (!logits || !lse || !top_ids || !top_logp || !workspace) return ULORL_ERR_INVALID_ARG;
+  if (!aligned16(logits) || T < 1 || T > 65536 || V < 4096 || V > kHeadMaxSize || top_k < 1 || top_k > ULORL_MAX_TOP)
+    return ULORL_ERR_INVALID_ARG;
+  if (limit_cycles < 1000 || limit_cycles > 100000000) return ULORL_ERR_INVALID_ARG;
+  RowsArgs a{};
+  a.logits = logits; a.ld = (size_t)V;
+  a.T = T; a.V = V; a.k = top_k;
+  a.kappa = 1.f;
+  a.lse = lse;
+  a.top_ids = top_ids; a.top_logp = top_logp;
+  a.status = static_cast<int*>(workspace);
+  a.wait_limit = limit_cycles;
+  return launch_rows<float, true>(a, device_sm_count(), reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
 int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
                       const int32_t* teacher_ids, const float* teacher_logp, const float* weights,
                       float* loss, float* kl, float* lse, float* norm, float* coef, float* entry_grad,
@@ -747,6 +764,7 @@ int ulorl_distill_fwd(const ulorl_head_params_t* params, const void* hidden, con
       a.T = rows; a.V = V;
       a.kappa = params->inv_temperature;
       a.partials = partials + t0;
+      a.status = status;
       st = launch_rows<float>(a, pl.sms, stream);
       if (st != ULORL_OK) return st;
     }

@@ -133,7 +133,8 @@ struct RowsArgs {
   int* top_ids;             // [T][k]
   float* top_logp;          // [T][k]
   float4* partials;         // (m, r, -, -) for a merge that follows
-  int* status;              // NULL: a target out of range gets a NaN
+  int* status;              // timeouts and targets out of range; NULL: their results are NaN, nothing is reported
+  long long wait_limit;     // kHeld only
 };
 
 constexpr int kRowThreads = 256;
@@ -270,7 +271,8 @@ __device__ __forceinline__ RowSums merge_lanes(float m, float s, float u, int n,
 // maximum is: only their few vectors are read again.
 // Bound by issue slots (about ten instructions an entry): 4096 rows of 151936 bf16 take 247 us, 5.0 TB/s of the 6.5 that a copy
 // does, and 294 us with 8 alternatives; one row of float32 takes 10 us, 257 rows of 32003 float16 with 20 alternatives 12.
-template <typename T>
+// kHeld (the self-test of the bounded waits): the copies are never issued, and a wait gives up after args.wait_limit cycles.
+template <typename T, bool kHeld = false>
 __global__ void __launch_bounds__(kRowThreads, 4)
 logits_rows_kernel(const RowsArgs args) {
   namespace cg = cooperative_groups;
@@ -357,7 +359,9 @@ logits_rows_kernel(const RowsArgs args) {
   // The slice streams through a ring of three 16 KB batches that the copy engine fills (192 KB in flight on an SM with
   // four blocks).  A batch's slot is filled again one batch after it was read, by then by all warps.
   const int n_batch = (nvec + kRowBatch - 1) / kRowBatch;
+  const long long wait_limit = kHeld ? args.wait_limit : kWaitLimitCycles;
   auto refill = [&](int i) {                                        // thread 0
+    if (kHeld) return;
     const uint32_t bytes = (uint32_t)min(kRowBatch, nvec - i * kRowBatch) * 16u, bar = ptx::smem_u32(&bar_full[i % kRowStages]);
     ptx::mbar_arrive_expect_tx(bar, bytes);
     ptx::bulk_load(ring + (uint32_t)(i % kRowStages) * kRowBatch * 16u, vecs + (size_t)i * kRowBatch, bytes, bar);
@@ -367,7 +371,7 @@ logits_rows_kernel(const RowsArgs args) {
   for (int i = 0; i < n_batch; ++i) {
     const int stage = i % kRowStages, b = i * kRowBatch;
     if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(ptx::smem_u32(&bar_full[stage]), (uint32_t)(i / kRowStages) & 1u, &abort_flag,
-                                                        kWaitLimitCycles)))
+                                                        wait_limit)))
       break;
     uint4 v[kRowUnroll];
     const uint4* src = ring_ptr + stage * kRowBatch + tid;
@@ -382,7 +386,7 @@ logits_rows_kernel(const RowsArgs args) {
     if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar_empty[stage]));
     if (tid == 0 && i > 0 && i - 1 + kRowStages < n_batch) {
       const int last = (i - 1) % kRowStages;
-      if (ptx::mbar_wait_bounded(ptx::smem_u32(&bar_empty[last]), (uint32_t)((i - 1) / kRowStages) & 1u, &abort_flag, kWaitLimitCycles))
+      if (ptx::mbar_wait_bounded(ptx::smem_u32(&bar_empty[last]), (uint32_t)((i - 1) / kRowStages) & 1u, &abort_flag, wait_limit))
         refill(i - 1 + kRowStages);
     }
     __syncwarp();
@@ -409,14 +413,18 @@ logits_rows_kernel(const RowsArgs args) {
   }
   if (tid == 0) { n_owner = 0; n_cand = 0; }
   __syncthreads();
+  const bool gave_up = abort_flag != 0;                             // the same in all threads: nobody waits any more
+  if (gave_up && tid == 0 && args.status) atomicOr(args.status, kStatusTimeout);
   if (warp == 0) {
     const bool on = lane < kWarps;
     const RowSums all = merge_lanes(on ? sh_m[lane] : -INFINITY, on ? sh_s[lane] : 0.f, on ? sh_u[lane] : 0.f, on ? sh_n[lane] : 0, c2);
     if (lane == 0) { sh_mine.m = all.m; sh_mine.r = all.r; sh_mine.u = all.u; sh_mine.owners = all.owners; }
   }
 
-  // ---- the slice's k largest, falling, into sh_mine.top
-  if (k > 0) {
+  // ---- the slice's k largest, falling, into sh_mine.top; none where a copy never came
+  if (gave_up) {
+    if (tid < kMaxTop) sh_mine.top[tid] = 0ull;
+  } else if (k > 0) {
     const bool holds = tid < nvec || tid < extras;
     const uint32_t mine = holds ? (order_key(st.lane_max) >> kShift) : 0u;
     // The lanes' places by their maxima: each warp sorts its 32 (shuffles), and every entry then looks up in the other

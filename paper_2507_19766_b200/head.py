@@ -254,6 +254,21 @@ def logits_scores(logits: torch.Tensor, targets=None, top_k: int = 0, inv_temper
     return out
 
 
+def selftest_logits_wait(logits: torch.Tensor, top_k: int, workspace: torch.Tensor, limit_cycles: int = 1_000_000) -> ScoresOut:
+    """ulorl_selftest_logits_wait on float32 logits [T, V]: lse and alternatives of a kernel whose waits ran out; the timeout
+    shows up in binding.check_status(workspace)."""
+    device = _device_of(logits, "logits")
+    T, V = logits.shape
+    pl, pws = _take(logits, "logits", torch.float32, T * V, device), _take(workspace, "workspace", torch.uint8, workspace.numel(), device)
+    lse, (ids, top_logp) = torch.empty(T, device=logits.device), _alternatives(T, top_k, logits)
+    with torch.cuda.device(device):
+        code = load_library().ulorl_selftest_logits_wait(pl, T, V, top_k, lse.data_ptr(), None if ids is None else ids.data_ptr(),
+                                                         None if ids is None else top_logp.data_ptr(), pws, limit_cycles, _stream(device))
+    if code != OK:
+        _raise(code, "ulorl_selftest_logits_wait")
+    return ScoresOut(None, None, lse, None, ids, top_logp)
+
+
 def distill_fwd(p: HeadParams, hidden, W, teacher_ids, teacher_logp, weights=None, out: Optional[DistillOut] = None,
                 workspace: Optional[torch.Tensor] = None) -> DistillOut:
     """ulorl_distill_fwd: loss of the student's softmax against the teacher's top_k entries per token."""

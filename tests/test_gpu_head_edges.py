@@ -141,3 +141,22 @@ def test_nan_columns_beside_alternatives():
         ref = R.scores64(R.logits64(h, w, 1.0), None, k)     # all sums are exact
         assert torch.equal(ids[1], ref["top_ids"].cpu())
         assert torch.equal(ids[0], ref["top_ids"].cpu())
+
+
+# ------------------------------------------------------------------------------------------------ failure reports
+@pytest.mark.parametrize("T,V", [(1, 200_000), (3, 5000), (700, 20_000)])
+def test_rows_report_a_wait_that_ran_out(T, V):
+    """The row kernel with copies that are never issued: its waits give up after their limit, the kernel returns, the status
+    word says so, and no number is made of what shared memory happened to hold."""
+    logits = torch.randn(T, V, generator=torch.Generator(device=DEV).manual_seed(V), device=DEV)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    U.logits_scores(logits, top_k=8)                         # leaves numbers in shared memory
+    out = U.head.selftest_logits_wait(logits, 8, ws, 100_000)
+    assert B.check_status(ws) == -5
+    assert bool(torch.isnan(out.lse).all())
+    assert bool((out.top_ids == -1).all()) and bool(torch.isnan(out.top_logp).all())
+    for bad in (10, 10 ** 12):
+        with pytest.raises(U.UlorlError):
+            U.head.selftest_logits_wait(logits, 8, ws, bad)
+    again = U.logits_scores(logits, top_k=8)                 # and the next call is an ordinary one
+    assert torch.equal(again.top_logp, U.logits_scores(logits, top_k=8).top_logp) and bool(torch.isfinite(again.lse).all())
