@@ -282,7 +282,7 @@ static int run_sgemm(const HeadPlan& pl, const float* A, size_t lda, const float
   a.ldc = parts > 1 ? (size_t)N : ldc;
   a.part_stride = parts > 1 ? (size_t)M * (size_t)N : 0;
   a.accumulate = parts > 1 ? 0 : accumulate;
-  const dim3 grid((N + kSgTile - 1) / kSgTile, (M + kSgTile - 1) / kSgTile, parts);
+  const dim3 grid(tile_blocks(M, N, kSgTile), 1, parts);
   sgemm_kernel<kAAlongK, kBAlongK><<<grid, kSgThreads, 0, stream>>>(a);
   ULORL_LAUNCH_CHECK();
   if (parts > 1) {                                                  // rows of the result are contiguous here: ldc = N
@@ -300,7 +300,7 @@ static int simt_logits_panel(const ulorl_head_params_t* p, const HeadPlan& pl, c
   if (p->dtype == ULORL_F32)
     return run_sgemm<true, true>(pl, static_cast<const float*>(hidden) + (size_t)t0 * H, H, static_cast<const float*>(W), H, panel, ld,
                                  rows, p->V, p->H, 0, nullptr, stream);
-  const dim3 grid((p->V + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
+  const unsigned grid = tile_blocks(rows, p->V, kSimtTile);
   simt_gemm_kernel<__nv_bfloat16, __nv_bfloat16, float><<<grid, kSimtThreads, 0, stream>>>(
       static_cast<const __nv_bfloat16*>(hidden) + (size_t)t0 * H, H, 1, static_cast<const __nv_bfloat16*>(W), 1, H, panel, ld, rows,
       p->V, p->H, 0);
@@ -533,8 +533,7 @@ static int run_head_bwd(const ulorl_head_params_t* p, const HeadPlan& pl, const 
       const int rows = std::min(T - t0, pl.panel_tokens);
       const int acc = (panel > 0 || acc_into) ? 1 : 0;
       const dim3 gdz((unsigned)std::min((V + 1023) / 1024, 64), rows);
-      const dim3 gdh((H + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
-      const dim3 gdw((H + kSimtTile - 1) / kSimtTile, (V + kSimtTile - 1) / kSimtTile);
+      const unsigned gdh = tile_blocks(rows, H, kSimtTile), gdw = tile_blocks(V, H, kSimtTile);
       const bool f32 = p->dtype == ULORL_F32;
       st = simt_logits_panel(p, pl, hidden, W, t0, rows, dz, ld, stream);
       if (st != ULORL_OK) return st;

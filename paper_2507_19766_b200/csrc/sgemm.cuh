@@ -12,6 +12,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "simt.cuh"
 #include "umma_gemm.cuh"
 
 namespace ulorl {
@@ -75,7 +76,8 @@ __global__ void __launch_bounds__(kSgThreads)
 sgemm_kernel(const SgemmArgs a) {
   __shared__ __align__(16) float As[2][kSgK][kSgTile + kSgPad];
   __shared__ __align__(16) float Bs[2][kSgK][kSgTile + kSgPad];
-  const int m0 = blockIdx.y * kSgTile, n0 = blockIdx.x * kSgTile;
+  int m0, n0;
+  tile_of_block(a.N, kSgTile, m0, n0);
   const int k_begin = blockIdx.z * a.k_part, k_end = min(a.K, k_begin + a.k_part);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   float2 acc[8][4] = {};

@@ -186,7 +186,18 @@ simt_dz_kernel(const TIn* __restrict__ hidden, const TIn* __restrict__ W, const 
   }
 }
 
-// C[m, n] (+)= sum_k A(m, k) * B(k, n) with arbitrary element strides; float32 accumulate.
+// Blocks of a contraction with M x N outputs in square tiles, columns fastest, all along x: a grid's other dimensions end at
+// 65535, and d_W has the vocabulary on its rows (a vocabulary of 4.2 million has that many tiles of 64).
+inline unsigned tile_blocks(int M, int N, int tile) {
+  return (unsigned)((size_t)((M + tile - 1) / tile) * (size_t)((N + tile - 1) / tile));
+}
+__device__ __forceinline__ void tile_of_block(int N, int tile, int& row0, int& col0) {
+  const unsigned columns = (unsigned)((N + tile - 1) / tile);
+  row0 = (int)(blockIdx.x / columns) * tile;
+  col0 = (int)(blockIdx.x % columns) * tile;
+}
+
+// C[m, n] (+)= sum_k A(m, k) * B(k, n) with arbitrary element strides; float32 accumulate.  Grid: tile_blocks.
 template <typename TA, typename TB, typename TC>
 __global__ void __launch_bounds__(kSimtThreads)
 simt_gemm_kernel(const TA* __restrict__ A, size_t a_sm, size_t a_sk, const TB* __restrict__ B, size_t b_sk,
@@ -195,7 +206,8 @@ simt_gemm_kernel(const TA* __restrict__ A, size_t a_sm, size_t a_sk, const TB* _
   __shared__ float Bs[kSimtBK][kSimtTile + 1];
   const int tid = threadIdx.x;
   const int tx = tid & 15, ty = tid >> 4;
-  const int row0 = blockIdx.y * kSimtTile, col0 = blockIdx.x * kSimtTile;
+  int row0, col0;
+  tile_of_block(N, kSimtTile, row0, col0);
   float acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)

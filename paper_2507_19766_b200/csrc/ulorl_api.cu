@@ -889,8 +889,7 @@ static int bwd_impl(const ulorl_params_t* params, const void* hidden, const void
   for (int t0 = 0, panel = 0; t0 < T; t0 += pl.panel_tokens, ++panel) {
     const int rows = (T - t0) < pl.panel_tokens ? (T - t0) : pl.panel_tokens;
     const dim3 gdz((rows + kSimtTile - 1) / kSimtTile, (V + kSimtTile - 1) / kSimtTile);
-    const dim3 gdh((H + kSimtTile - 1) / kSimtTile, (rows + kSimtTile - 1) / kSimtTile);
-    const dim3 gdw((H + kSimtTile - 1) / kSimtTile, (V + kSimtTile - 1) / kSimtTile);
+    const unsigned gdh = tile_blocks(rows, H, kSimtTile), gdw = tile_blocks(V, H, kSimtTile);
     const int acc = (panel > 0 || acc_into) ? 1 : 0;
     if (params->dtype == ULORL_F32) {
       const float* h = static_cast<const float*>(hidden);

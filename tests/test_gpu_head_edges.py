@@ -160,3 +160,19 @@ def test_rows_report_a_wait_that_ran_out(T, V):
             U.head.selftest_logits_wait(logits, 8, ws, bad)
     again = U.logits_scores(logits, top_k=8)                 # and the next call is an ordinary one
     assert torch.equal(again.top_logp, U.logits_scores(logits, top_k=8).top_logp) and bool(torch.isfinite(again.lse).all())
+
+
+# ------------------------------------------------------------------------------------------------ sizes
+@pytest.mark.parametrize("dtype,V", [("bf16", 64 * 65535 + 1), ("f32", 128 * 65535 + 1)])
+def test_vocabulary_of_millions_on_cuda_cores(dtype, V):
+    """More tiles of d_W than one dimension of a grid other than the first takes."""
+    T, H = 2, 8
+    g = torch.Generator(device=DEV).manual_seed(1)
+    hidden, W = torch.randn(T, H, generator=g, device=DEV).to(DT[dtype]), torch.randn(V, H, generator=g, device=DEV).to(DT[dtype])
+    targets = torch.tensor([3, V - 1], dtype=torch.int32, device=DEV)
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, kernel_path="simt")
+    out = U.token_scores(p, hidden, W, targets)
+    d = torch.tensor([1.0, -2.0], device=DEV)
+    d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d, None)
+    dz, size = R.scores_dz64(R.logits64(hidden, W, 1.0), targets, 1.0, d, None)
+    R.check_grads(d_h, d_W, dz, size, hidden, W, R.logit_error(hidden, W, 1.0) * 2, False, "f32")
