@@ -801,6 +801,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_scores_kernel(const Me
 // ------------------------------------------------------------------------------------------ gradients of scores
 // (m, log2 s, alpha, beta) and the value at the target's column for the dz pass:
 //   dz_j = kappa g (1[j = y] - p_j) - kappa e p_j (log p_j + H) = 2^L (alpha + beta L) off the target, L = log2 p_j.
+// A zero gradient takes its factor out: the log-prob and entropy of a padding row may be NaN.
 __global__ void row_params_kernel(int T, float kappa, const float2* __restrict__ norm, const float* __restrict__ logp,
                                   const float* __restrict__ entropy, const float* __restrict__ d_logp,
                                   const float* __restrict__ d_entropy, float4* __restrict__ row_p, float* __restrict__ row_ins) {
@@ -809,10 +810,10 @@ __global__ void row_params_kernel(int T, float kappa, const float2* __restrict__
   const float g = d_logp ? d_logp[t] : 0.f, e = d_entropy ? d_entropy[t] : 0.f;
   const float H = d_entropy ? entropy[t] : 0.f;
   const float2 n = norm[t];
-  row_p[t] = make_float4(n.x, n.y * kLog2e, -kappa * fmaf(e, H, g), -kappa * e * kLn2);
+  row_p[t] = make_float4(n.x, n.y * kLog2e, -kappa * (e != 0.f ? fmaf(e, H, g) : g), -kappa * e * kLn2);
   if (d_logp) {
     const float l = logp[t];
-    row_ins[t] = kappa * (-expm1f(l) * g - (e != 0.f ? expf(l) * e * (l + H) : 0.f));
+    row_ins[t] = kappa * ((g != 0.f ? -expm1f(l) * g : 0.f) - (e != 0.f ? expf(l) * e * (l + H) : 0.f));
   }
 }
 

@@ -176,3 +176,30 @@ def test_vocabulary_of_millions_on_cuda_cores(dtype, V):
     d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d, None)
     dz, size = R.scores_dz64(R.logits64(hidden, W, 1.0), targets, 1.0, d, None)
     R.check_grads(d_h, d_W, dz, size, hidden, W, R.logit_error(hidden, W, 1.0) * 2, False, "f32")
+
+
+# ------------------------------------------------------------------------------------------------ gradients of scores
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("which", ["both", "logp", "entropy"])
+def test_rows_without_gradients_add_nothing(dtype, path, which):
+    """Padding rows with finite hidden states whose logits overflow: scores of NaN, gradients of zero, and nothing of them in
+    d_hidden and d_W."""
+    T, H, V = 70, 64, 500
+    hidden, W, targets = operands(T, H, V, dtype, seed=6)
+    pad = torch.arange(T, device=DEV) % 5 == 2
+    hidden[pad] = 3e38 if dtype == "bf16" else 1e38
+    W[::3] = 4.0
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, kernel_path=path)
+    out = U.token_scores(p, hidden, W, targets)
+    assert bool(torch.isnan(out.logp[pad]).any()) and bool(torch.isnan(out.entropy[pad]).all()) and bool(torch.isfinite(out.logp[~pad]).all())
+    g = torch.Generator().manual_seed(7)
+    d_logp, d_ent = (torch.randn(T, generator=g).to(DEV).masked_fill(pad, 0.0) for _ in range(2))
+    d_logp, d_ent = d_logp if which != "entropy" else None, d_ent if which != "logp" else None
+    d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d_logp, d_ent)
+    assert not bool(d_h[pad].any())
+    # the same without the rows
+    q = U.HeadParams(T=int((~pad).sum()), H=H, V=V, dtype=dtype, kernel_path=path)
+    h, y = hidden[~pad].contiguous(), targets[~pad].contiguous()
+    dz, size = R.scores_dz64(R.logits64(h, W, 1.0), y, 1.0, None if d_logp is None else d_logp[~pad], None if d_ent is None else d_ent[~pad])
+    R.check_grads(d_h[~pad], d_W, dz, size, h, W, R.logit_error(h, W, 1.0) * (2 + math.log(V)), dtype == "bf16" and path != "simt", "f32")
+    assert q.T < T
