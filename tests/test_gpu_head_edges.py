@@ -203,3 +203,33 @@ def test_rows_without_gradients_add_nothing(dtype, path, which):
     dz, size = R.scores_dz64(R.logits64(h, W, 1.0), y, 1.0, None if d_logp is None else d_logp[~pad], None if d_ent is None else d_ent[~pad])
     R.check_grads(d_h[~pad], d_W, dz, size, h, W, R.logit_error(h, W, 1.0) * (2 + math.log(V)), dtype == "bf16" and path != "simt", "f32")
     assert q.T < T
+
+
+@pytest.mark.parametrize("level", [40.0, 640.0, 5600.0])
+def test_dz_of_large_logits_keeps_its_scale(level):
+    """bf16 operands, logits of `level` plus fractions: dz, read back through hidden states of one 1 each, rounds the exact
+    values to bf16, with no common factor of a row beside the rounding."""
+    T, H, V = 40, 48, 40000
+    g = torch.Generator().manual_seed(int(level))
+    W, hidden = torch.zeros(V, H), torch.zeros(T, H)
+    hidden[:, :2] = 1.0
+    hidden[torch.arange(T), 8 + torch.arange(T)] = 1.0
+    W[:, 0] = level
+    W[:, 1] = torch.randint(0, 8, (V,), generator=g).float() * 2.0 ** -11       # sums are exact: multiples of 2^-11 below 2^13
+    W[:, 8:] = torch.randint(0, 256, (V, H - 8), generator=g).float() * 2.0 ** -8
+    targets = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).to(DEV)
+    h, w = hidden.to(torch.bfloat16).to(DEV), W.to(torch.bfloat16).to(DEV)
+    p = U.HeadParams(T=T, H=H, V=V)
+    out = U.token_scores(p, h, w, targets)
+    d_logp = (torch.rand(T, generator=g) + 0.5).to(DEV)
+    _, d_W = U.token_scores_bwd(p, h, w, targets, out, d_logp, None)
+    got = d_W[:, 8:].t().double()                            # [T, V]: dz times one
+    dz, _ = R.scores_dz64(R.logits64(h, w, 1.0), targets, 1.0, d_logp, None)
+    # A value is relatively off by less than 2^-16 before its rounding: exponents of up to 17 that are rounded (2^-20) after the
+    # logarithm of the sum (2^-19 with its own rounding), ex2 2^-22, and, where the row's constant is one number, two roundings of
+    # a number below 128 (2^-17 ln 2).  Rounding to bf16 keeps the order, so a row's sum lies between those of the two ends.
+    eps = 2.0 ** -16
+    off = torch.ones_like(dz).scatter_(1, targets.long()[:, None], 0.0)         # the target's column is set on its own
+    low, high = (((dz * s).float().to(torch.bfloat16).double() * off).sum(1) for s in (1 + eps, 1 - eps))
+    total = (got * off).sum(1)
+    assert bool((total >= low).all()) and bool((total <= high).all()), float(((total - (low + high) / 2) / total).abs().max())
