@@ -1063,8 +1063,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       // beta = 0: alpha goes into the exponent, c2 a + k_row.  What rounding takes off k_row is a factor that a row's entries
       // share, so unlike their rounding to bf16 it does not average out: for |c2 m| up to 64 (logits up to 44, those of
       // trained heads) it is at most 2^-17, next to what the row's statistics carry; beyond, the difference to m is taken first.
+      // (One form for a warp's rows; rows without a gradient, padding among them, have no say.)
       [[maybe_unused]] bool flat = false;
-      if (kMode == kModeDzRow) flat = args.row_flat && !__any_sync(0xffffffffu, fabsf(rp.x * c2) > 64.f);
+      if (kMode == kModeDzRow) flat = args.row_flat && !__any_sync(0xffffffffu, rp.z != 0.f && fabsf(rp.x * c2) > 64.f);
       if (kMode == kModeDz) {
         if (row_ok) {
           const float gl = args.grad_loss ? *args.grad_loss : 1.f;

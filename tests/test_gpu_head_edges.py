@@ -205,6 +205,32 @@ def test_rows_without_gradients_add_nothing(dtype, path, which):
     assert q.T < T
 
 
+@pytest.mark.parametrize("dtype,path", PATHS)
+@pytest.mark.parametrize("mode", ["raw", "renorm", "tail"])
+def test_tokens_that_are_not_trained_on_add_nothing(dtype, path, mode):
+    """Padding rows with finite hidden states whose logits overflow, of weight zero or with an empty list."""
+    T, H, V, K = 70, 64, 500, 6
+    hidden, W, _ = operands(T, H, V, dtype, seed=8)
+    W[::3] = 4.0
+    g = torch.Generator().manual_seed(9)
+    ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(T)]).to(torch.int32).to(DEV)
+    teacher = (torch.log_softmax(torch.randn(T, K, generator=g), 1) - 0.2).to(DEV)
+    weights = torch.ones(T, device=DEV)
+    light, empty = torch.arange(T, device=DEV) % 5 == 2, torch.arange(T, device=DEV) % 7 == 3
+    weights[light] = 0.0
+    ids[empty] = -1
+    p = U.HeadParams(T=T, H=H, V=V, dtype=dtype, top_k=K, distill_mode=mode, kernel_path=path)
+
+    def step():
+        out = U.distill_fwd(p, hidden, W, ids, teacher, weights)
+        return (out.loss, *U.distill_bwd(p, hidden, W, ids, out))
+    want = step()
+    hidden[light | empty] = 3e38 if dtype == "bf16" else 1e38
+    got = step()
+    assert not bool(got[1][light | empty].any())
+    assert bool(torch.isfinite(got[0]).all()) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("level", [40.0, 640.0, 5600.0])
 def test_dz_of_large_logits_keeps_its_scale(level):
     """bf16 operands, logits of `level` plus fractions: dz, read back through hidden states of one 1 each, rounds the exact
