@@ -259,3 +259,57 @@ def test_dz_of_large_logits_keeps_its_scale(level):
     low, high = (((dz * s).float().to(torch.bfloat16).double() * off).sum(1) for s in (1 + eps, 1 - eps))
     total = (got * off).sum(1)
     assert bool((total >= low).all()) and bool((total <= high).all()), float(((total - (low + high) / 2) / total).abs().max())
+
+
+# ------------------------------------------------------------------------------------------------ planes of float32 operands
+def planes(x):
+    out = []
+    for _ in range(3):
+        out.append(x.float().to(torch.bfloat16).double())
+        x = x.double() - out[-1]
+    return out
+
+
+def without(x, y, product):
+    """x y as five of the six products of their planes."""
+    a, b = planes(x), planes(y)
+    return sum(a[i] * b[j] for i, j in ((0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0)) if (i, j) != product)
+
+
+@pytest.mark.parametrize("single", ["hidden", "W"])
+def test_each_product_of_planes_counts(single):
+    """Contractions of one product of two float32 numbers each, where every one of the six products of planes shows: with
+    hidden diagonal the logits and d_W are that, with W diagonal the logits and d_hidden."""
+    n = 40
+    g = torch.Generator().manual_seed(5)
+    full, diag = 0.25 + 0.25 * torch.rand(n, n, generator=g), 1.0 + torch.rand(n, generator=g)
+    hidden, W = (torch.diag(diag), full) if single == "hidden" else (full, torch.diag(diag))
+    hidden, W = hidden.to(DEV), W.to(DEV)
+    targets = torch.randint(0, n, (n,), generator=g, dtype=torch.int32).to(DEV)
+    d_logp = (torch.rand(n, generator=g) + 0.5).to(DEV)
+    p = U.HeadParams(T=n, H=n, V=n, dtype="f32", kernel_path="tensor")
+    out = U.token_scores(p, hidden, W, targets)
+    d_h, d_W = U.token_scores_bwd(p, hidden, W, targets, out, d_logp, None)
+    z = R.logits64(hidden, W, 1.0)
+    dz, _ = R.scores_dz64(z, targets, 1.0, d_logp, None)
+    far = lambda got, want: float(((got - want).abs() / want.abs()).max())
+    # a logit: the last sum cut off by at most 2^-23, the products left out 2 * 2^-24; twice that, for the small sums too
+    tol = 2.0 ** -21
+    if single == "hidden":
+        x, y = hidden.diag()[:, None].cpu(), W.t().cpu()                        # z[t, v] = hidden[t, t] W[v, t]
+    else:
+        x, y = hidden.cpu(), W.diag()[None, :].cpu()                            # z[t, v] = hidden[t, v] W[v, v]
+    assert far(out.norm[:, 0].double(), z.amax(1)) <= tol
+    # dz: logits below 1 off by 2^-22 each, ln of the sum (3.7) and its product with log2 e to 2^-22 each with their roundings,
+    # an exponent of up to 6 rounded, ex2 2^-22, the sum 2^-22: below 3.5 * 2^-21; then a product as above
+    grad = 2.0 ** -19
+    if single == "hidden":
+        a, b, got = dz.t().cpu(), hidden.diag()[None, :].cpu(), d_W             # d_W[v, h] = dz[h, v] hidden[h, h]
+    else:
+        a, b, got = dz.cpu(), W.diag()[None, :].cpu(), d_h                      # d_hidden[t, h] = dz[t, h] W[h, h]
+    b = b.double().expand_as(a)
+    assert far(got.double().cpu(), a * b) <= grad
+    # and each of the products is more than that
+    for product in ((0, 2), (2, 0), (1, 1), (0, 1), (1, 0)):
+        assert far(without(x.double(), y.double(), product).amax(1), (x.double() * y.double()).amax(1)) > tol, product
+        assert far(without(a, b, product), a * b) > grad, product
