@@ -313,3 +313,24 @@ def test_each_product_of_planes_counts(single):
     for product in ((0, 2), (2, 0), (1, 1), (0, 1), (1, 0)):
         assert far(without(x.double(), y.double(), product).amax(1), (x.double() * y.double()).amax(1)) > tol, product
         assert far(without(a, b, product), a * b) > grad, product
+
+
+# ------------------------------------------------------------------------------------------------ paths
+@pytest.mark.parametrize("T,H,V", [(8, 336, 2993), (100, 64, 900), (60, 128, 4000), (1, 256, 5000)])
+@pytest.mark.parametrize("path", ["auto", "simt", "tensor"])
+def test_entropy_gradients_of_peaked_rows(T, H, V, path):
+    """float32 operands, gradients of the entropy alone, rows that are sharply peaked: what AUTO takes of itself for the two
+    calls belongs together, so a gradient of 10^-8 is not lost beside the difference of two paths' logits."""
+    hidden, W, targets = operands(T, H, V, "f32", seed=T + V)
+    g = torch.Generator().manual_seed(3)
+    rows = torch.arange(T) % 3 != 1
+    hidden[rows] += (W[targets.long()] * (64.0 * 24 / H))[rows]
+    d_ent = torch.randn(T, generator=g).to(DEV)
+    p = U.HeadParams(T=T, H=H, V=V, dtype="f32", kernel_path=path)
+    ws = U.alloc_head_workspace(p, DEV)
+    out = U.token_scores(p, hidden, W, targets, workspace=ws)
+    d_h, d_W = U.token_scores_bwd(p, hidden, W, None, out, None, d_ent, workspace=ws)
+    z = R.logits64(hidden, W, 1.0)
+    dz, size = R.scores_dz64(z, targets, 1.0, None, d_ent)
+    assert float(R.scores64(z, targets)["entropy"].min()) < 1e-5
+    R.check_grads(d_h, d_W, dz, size, hidden, W, R.logit_error(hidden, W, 1.0) * (2 + math.log(V)), False, "f32")
