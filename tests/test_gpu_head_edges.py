@@ -334,3 +334,18 @@ def test_entropy_gradients_of_peaked_rows(T, H, V, path):
     dz, size = R.scores_dz64(z, targets, 1.0, None, d_ent)
     assert float(R.scores64(z, targets)["entropy"].min()) < 1e-5
     R.check_grads(d_h, d_W, dz, size, hidden, W, R.logit_error(hidden, W, 1.0) * (2 + math.log(V)), False, "f32")
+
+
+# ------------------------------------------------------------------------------------------------ many calls
+@pytest.mark.parametrize("T,V,k,dtype", [(4909, 60244, 31, torch.float32), (4096, 60001, 8, torch.bfloat16), (149, 400_000, 4, torch.float16)])
+def test_long_rows_are_read_once_and_whole(T, V, k, dtype):
+    """Rows of many batches, more blocks than the GPU runs at once: every call sees the same numbers, bit for bit."""
+    z = torch.randn(T, V, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).to(dtype)
+    y = torch.zeros(T, dtype=torch.int32, device=DEV)
+    first = U.logits_scores(z, y, top_k=k)
+    values = torch.sort(z, dim=1, descending=True).values[:, :k] if T * V < 3e8 else torch.topk(z, k, dim=1).values
+    assert torch.equal(z.gather(1, first.top_ids.long()), values)
+    for _ in range(100):
+        out = U.logits_scores(z, y, top_k=k)
+        for name in ("lse", "logp", "entropy", "top_ids", "top_logp"):
+            assert torch.equal(getattr(out, name), getattr(first, name)), name
