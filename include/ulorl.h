@@ -339,8 +339,8 @@ int ulorl_token_loss_step_host(const ulorl_params_t* params,
  * from a teacher's top logits.  All calls follow the conventions above: caller-owned device memory, no
  * synchronisation, device findings in the workspace status word, bit-identical results for equal inputs.  With
  *     a[t, v] = hidden[t] . W[v],  z = inv_temperature a,  p = softmax(z[t, :]),  lse = ln sum_v e^z
- * hidden [T,H], W [V,H] have the type `dtype`; the T x V logits are never written to global memory (CUDA-core
- * path: beyond one token panel of float32).  Float32 operands run on CUDA cores (SIMT) or, split into three bf16 planes
+ * hidden [T,H], W [V,H] have the type `dtype`; the T x V logits are not written to global memory, but for one panel of
+ * float32: a token panel on CUDA cores, all of them for up to 64 tokens of bf16 on the tensor cores.  Float32 operands run on CUDA cores (SIMT) or, split into three bf16 planes
  * that keep all 24 bits, on the tensor cores (TENSOR; finite operands below 3.3e38, the planes are 6 bytes an entry of workspace);
  * AUTO takes the faster one by the sizes (ulorl_token_scores_bwd with d_entropy: the one of its forward call).
  * Any T >= 0; H a multiple of 8; no size above 2^30.

@@ -70,6 +70,8 @@ static int sgemm_parts(const HeadPlan& pl, int M, int N, int K, int* k_part) {
 // Whether float32 operands go through the tensor cores: six products of bf16 planes against CUDA-core multiply-adds.
 // Modelled microseconds of a forward call per 10^6 of V x H, and what the planes cost a small one (measured 39 us for 43 at
 // 512 tokens x 4096, H 256; 31 for 29 at 512 x 1000, H 128; 199 for 254 at 1 x 32768, H 1024; 209 for 881 at 512 tokens).
+// V x H counts columns as they are, planes are padded to a multiple of 128: at H 64 and below the tensor path does twice the work
+// and more of what is modelled here.
 static bool split_pays(const ulorl_head_params_t* p, bool backward) {
   if (!split_possible(p)) return false;
   const double vh = 1e-6 * (double)p->V * (double)p->H;
@@ -87,7 +89,7 @@ constexpr int kSplitPanel = 2048, kSplitTokens = 512, kSplitEntries = 2048;
 
 // as_forward: the backward call takes the path that the forward call takes of itself.  A gradient of entropies needs it: at
 // the maximum of a peaked row dz is -e p (ln p + H) with ln p = -10^-8, and the other path's logit there is 10^-6 off the
-// maximum that the forward call saved (d_hidden of 8 tokens x 2993, H 336 10^-5 off in all, 5 * 10^-7 with one path).
+// maximum that the forward call saved (d_hidden of 8 tokens x 2993, H 336 10^-5 off in all, 2.4 * 10^-6 with one path).
 // Gradients of log-probs have no such difference in them.
 static HeadPlan make_head_plan(const ulorl_head_params_t* p, bool backward, bool as_forward = false) {
   HeadPlan pl{};
@@ -153,7 +155,8 @@ static HeadPlan make_head_plan(const ulorl_head_params_t* p, bool backward, bool
   // unit; units of 256 x 256 can.  d_hidden reduces over the vocabulary and its epilogue is small: 512, unless a
   // quarter or more of the columns would be padding.  d_W reduces over the panel's tokens; measured with 512 and with
   // 256 columns, at 151936 x 2048: 64 tokens 184 and 216 us, 200 tokens 282 and 292, 2011 tokens 1072 and 980, 8192 tokens
-  // 3990 and 3750; 50000 x 256, 2000 tokens: 74 and 51.
+  // 3990 and 3750; 50000 x 256, 2000 tokens: 74 and 51.  These are of d_W in bf16, before its epilogue had two groups of warps;
+  // for float32 d_W and one that is added into the rule is the same and was not measured.
   const size_t h1 = align_up((size_t)H, kBN), h2 = align_up((size_t)H, 2 * kBN);
   pl.dh_acc = 4 * h2 >= 5 * h1 ? 1 : 2;
   pl.dw_acc_tiles = panel > 512 || 4 * h2 >= 5 * h1 ? 1 : 2;
@@ -356,8 +359,8 @@ static int logits_panel(const ulorl_head_params_t* p, const HeadPlan& pl, const 
   return launch_small<64>(p, pl, hidden, W, logits, status, stream);
 }
 
-// Rows are spread over clusters until there are two blocks a multiprocessor, as long as a block keeps four loads a
-// thread; more than eight blocks a cluster have to be asked for, once per device.
+// Rows are spread over clusters until there are two blocks a multiprocessor (four fit; the rule is older), as long as a
+// block keeps four loads a thread; more than eight blocks a cluster have to be asked for, once per device.
 template <typename T, bool kHeld = false>
 static int launch_rows(const RowsArgs& a, int sms, cudaStream_t stream) {
   static bool opted_in[kMaxDevices] = {};

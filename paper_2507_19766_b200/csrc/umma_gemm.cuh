@@ -18,6 +18,11 @@
 //   kModeDWBf16  d_W rounded to bf16 in the epilogue (all tokens in one launch)
 //   kModeDzRow3  kModeDzRow with dz written as three bf16 planes
 //
+// Of bf16 operands two things are held in fewer bits than a float32 form would, by choice.  dz leaves its kernel as bf16,
+// what the two gradient contractions take (as two planes they would cost twice as much): d_hidden and d_W are 2.4e-3 of the
+// whole off where rounding them alone gives 1.7e-3 (CUDA-core path: dz in float32).  And a logit is one float32 sum over H that
+// the tensor core cuts off rather than rounds: entropy and kl at H 2048 are 2e-6 off where a float32 product is 0.5e-6 off.
+//
 // Float32 operands of scoring and distillation come as three bf16 planes x = h + m + l (24 bits, see split_planes_kernel)
 // side by side in the rows of a matrix, and a contraction runs over six products of planes: what is left out, m l and
 // smaller, is 2^-24 of the whole.  hh comes last, so that the accumulator is small while the small products are added.
@@ -25,9 +30,10 @@
 // take 6.9; log-probs 1e-7 and gradients 1e-6 off (relative to the whole).
 //
 // One kernel template umma_kernel<mode, CTAs per MMA, accumulators per unit>, persistent, one CTA per
-// SM, 192 threads: one thread of warp 0 feeds a shared-memory ring with TMA tile loads (128-byte
-// swizzle), one thread of warp 1 issues tcgen05.mma into tensor memory, warps 2-5 drain accumulators
-// with tcgen05.ld (one output row per thread) and run the mode's epilogue.
+// SM: one thread of warp 0 feeds a shared-memory ring with TMA tile loads (128-byte swizzle), one
+// thread of warp 1 issues tcgen05.mma into tensor memory, warps 2-5 drain accumulators with
+// tcgen05.ld (one output row per thread) and run the mode's epilogue.  192 threads; 320, with
+// epilogue warps 2-9, for kModeScores*, kModeDistill, kModeDzRow* and kModeDWBf16.
 //   <m, 2, 1>  CTA pair, one 256 x 256 MMA tile over both CTAs, two 256-column accumulator buffers: the
 //              epilogue of tile i overlaps the contraction of tile i + 1 (statistics, dz)
 //   <m, 2, 2>  CTA pair, 256 x 512 unit = two accumulators fed from the same A stage, tensor memory as
