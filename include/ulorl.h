@@ -340,9 +340,9 @@ int ulorl_token_loss_step_host(const ulorl_params_t* params,
  * synchronisation, device findings in the workspace status word, bit-identical results for equal inputs.  With
  *     a[t, v] = hidden[t] . W[v],  z = inv_temperature a,  p = softmax(z[t, :]),  lse = ln sum_v e^z
  * hidden [T,H], W [V,H] have the type `dtype`; the T x V logits are not written to global memory, but for one panel of
- * float32: a token panel on CUDA cores, all of them for up to 64 tokens of bf16 on the tensor cores.  Float32 operands run on CUDA cores (SIMT) or, split into three bf16 planes
- * that keep all 24 bits, on the tensor cores (TENSOR; finite operands below 3.3e38, the planes are 6 bytes an entry of workspace);
- * AUTO takes the faster one by the sizes (ulorl_token_scores_bwd with d_entropy: the one of its forward call).
+ * float32: a token panel on CUDA cores, all of them for up to 64 tokens of bf16 on the tensor cores.  Float32 operands run on
+ * CUDA cores (SIMT) or, split into three bf16 planes that keep all 24 bits, on the tensor cores (TENSOR; finite operands
+ * below 3.3e38, the planes are 6 bytes an entry of workspace); AUTO takes one by the sizes, for each call by itself.
  * Any T >= 0; H a multiple of 8; no size above 2^30.
  */
 typedef enum { ULORL_F16 = 2 } ulorl_logits_dtype_t;      /* further type of ulorl_logits_scores                   */
@@ -398,8 +398,7 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
  *   dz[t, v] = kappa (d_logp (1[v = y_t] - p_v) - d_entropy p_v (ln p_v + entropy)),
  *   d_hidden = dz W (params->dtype), d_W = dz^T hidden (params->dw_dtype, added into when params->dw_accumulate).
  * norm, logp and entropy are the outputs of ulorl_token_scores (logp and targets are read with d_logp, entropy with
- * d_entropy), of the same kernel_path where d_entropy is given: a sharply peaked row's gradient of the entropy is smaller
- * than what another path's logits differ by.  A row whose two gradients are zero adds nothing, whatever its softmax; its hidden state must be
+ * d_entropy).  A row whose two gradients are zero adds nothing, whatever its softmax; its hidden state must be
  * finite all the same.
  */
 int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden, const void* W,

@@ -87,15 +87,11 @@ static bool split_pays(const ulorl_head_params_t* p, bool backward) {
 // tokens would do for d_W, but leave d_hidden few units (2048 tokens x 32768, H 2048: 4.5 ms instead of 3.6).
 constexpr int kSplitPanel = 2048, kSplitTokens = 512, kSplitEntries = 2048;
 
-// as_forward: the backward call takes the path that the forward call takes of itself.  A gradient of entropies needs it: at
-// the maximum of a peaked row dz is -e p (ln p + H) with ln p = -10^-8, and the other path's logit there is 10^-6 off the
-// maximum that the forward call saved (d_hidden of 8 tokens x 2993, H 336 10^-5 off in all, 2.4 * 10^-6 with one path).
-// Gradients of log-probs have no such difference in them.
-static HeadPlan make_head_plan(const ulorl_head_params_t* p, bool backward, bool as_forward = false) {
+static HeadPlan make_head_plan(const ulorl_head_params_t* p, bool backward) {
   HeadPlan pl{};
   pl.planes = p->dtype == ULORL_F32 ? 3 : 1;
   pl.tensor = p->kernel_path == ULORL_PATH_TENSOR ||
-              (p->kernel_path != ULORL_PATH_SIMT && (p->dtype == ULORL_BF16 || split_pays(p, backward && !as_forward)));
+              (p->kernel_path != ULORL_PATH_SIMT && (p->dtype == ULORL_BF16 || split_pays(p, backward)));
   pl.width = pl.planes == 3 ? (int)align_up((size_t)p->H, 2 * kBK) : p->H;
   pl.sms = device_sm_count();
   pl.workers = std::max(1, pl.sms / 2);
@@ -588,8 +584,7 @@ extern "C" {
 size_t ulorl_head_workspace_bytes(const ulorl_head_params_t* params, int32_t backward) {
   if (validate_head(params) != ULORL_OK) return 0;
   const size_t fwd = make_head_plan(params, false).fwd_total;
-  if (!backward) return fwd;
-  return std::max(fwd, std::max(make_head_plan(params, true).bwd_total, make_head_plan(params, true, true).bwd_total));
+  return backward ? std::max(fwd, make_head_plan(params, true).bwd_total) : fwd;
 }
 
 int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, const void* W, const int32_t* targets,
@@ -668,7 +663,7 @@ int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden
   if (!norm || !d_hidden || !d_W || (!d_logp && !d_entropy)) return ULORL_ERR_INVALID_ARG;
   if ((d_logp && (!logp || !targets)) || (d_entropy && !entropy)) return ULORL_ERR_INVALID_ARG;
   if (!aligned16(d_hidden) || !aligned16(d_W) || !aligned8(norm)) return ULORL_ERR_UNSUPPORTED;
-  const HeadPlan pl = make_head_plan(params, true, d_entropy != nullptr);
+  const HeadPlan pl = make_head_plan(params, true);
   st = head_begin(hidden, W, workspace, workspace_bytes, pl.bwd_total, 0, stream);
   if (st != ULORL_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);

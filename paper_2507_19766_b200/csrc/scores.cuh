@@ -831,9 +831,10 @@ __global__ void dz_rows_f32_kernel(float* __restrict__ panel, size_t ld, int V, 
   const bool live = rp.z != 0.f || rp.w != 0.f;
   int y = -1;
   if (targets) y = min(max(targets[t], 0), V - 1);
-  const float c2 = kappa * kLog2e;
+  const float c2 = kappa * kLog2e, from = snap_from(rp, c2);
   for (int v = blockIdx.x * blockDim.x + threadIdx.x; v < V; v += gridDim.x * blockDim.x) {
-    const float L = fmaf(row[v] - rp.x, c2, -rp.y);
+    const float a = row[v];
+    const float L = fmaf((a > from ? rp.x : a) - rp.x, c2, -rp.y);
     float d = live ? exp2f(L) * fmaf(rp.w, L, rp.z) : 0.f;
     if (v == y) d = row_ins[t];
     row[v] = d;

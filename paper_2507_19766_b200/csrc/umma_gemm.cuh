@@ -317,11 +317,21 @@ __device__ __forceinline__ void dz_row_chunk(const uint32_t (&raw)[32], int nval
   }
 }
 
+// float32 operands: logits above this are the row's maximum itself, whatever the path that recomputes them.  The forward and
+// the backward call may have taken different ones, whose logits differ by 10^-6, and at the maximum of a peaked row the
+// gradient of an entropy is -e p (ln p + H) with ln p = -10^-8 (8 tokens x 2993, H 336: d_hidden 10^-5 off in all, 10^-6 with
+// this).  Where the others add up to less than a quarter of the maximum, each is more than two powers of two below it.
+__device__ __forceinline__ float snap_from(const float4& rp, float c2) {
+  return rp.y < 0.32f ? rp.x - 1.f / c2 : INFINITY;
+}
+
 // The same as float32, in place of the logits.
 __device__ __forceinline__ void dz_row_values(uint32_t (&raw)[32], int nvalid, float c2, const float4& rp, bool live) {
+  const float from = snap_from(rp, c2);
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
-    const float L = fmaf(__uint_as_float(raw[j]) - rp.x, c2, -rp.y);
+    const float a = __uint_as_float(raw[j]);
+    const float L = fmaf((a > from ? rp.x : a) - rp.x, c2, -rp.y);
     raw[j] = live && j < nvalid ? __float_as_uint(ex2f(L) * fmaf(rp.w, L, rp.z)) : 0u;
   }
 }

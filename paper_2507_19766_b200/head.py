@@ -191,7 +191,7 @@ def _grad_outputs(p: HeadParams, d_hidden, d_W, hidden, device: int):
 def token_scores_bwd(p: HeadParams, hidden, W, targets, scores: ScoresOut, d_logp=None, d_entropy=None, d_hidden=None,
                      d_W=None, workspace: Optional[torch.Tensor] = None):
     """ulorl_token_scores_bwd: (d_hidden, d_W) for d loss / d logp and d loss / d entropy (None = zero), given what
-    token_scores returned for the same operands (and kernel_path, with d_entropy)."""
+    token_scores returned for the same operands."""
     lib = load_library()
     cp = p.to_c()
     device, ph, pw = _operands(p, hidden, W)

@@ -317,19 +317,18 @@ def test_each_product_of_planes_counts(single):
 
 # ------------------------------------------------------------------------------------------------ paths
 @pytest.mark.parametrize("T,H,V", [(8, 336, 2993), (100, 64, 900), (60, 128, 4000), (1, 256, 5000)])
-@pytest.mark.parametrize("path", ["auto", "simt", "tensor"])
+@pytest.mark.parametrize("path", ["auto", "simt", "tensor", "simt-tensor", "tensor-simt"])
 def test_entropy_gradients_of_peaked_rows(T, H, V, path):
-    """float32 operands, gradients of the entropy alone, rows that are sharply peaked: what AUTO takes of itself for the two
-    calls belongs together, so a gradient of 10^-8 is not lost beside the difference of two paths' logits."""
+    """float32 operands, gradients of the entropy alone, rows that are sharply peaked: a gradient of 10^-8 is not lost beside
+    the difference of the logits of two paths, whichever the two calls take (auto: by the sizes, each for itself)."""
     hidden, W, targets = operands(T, H, V, "f32", seed=T + V)
     g = torch.Generator().manual_seed(3)
     rows = torch.arange(T) % 3 != 1
     hidden[rows] += (W[targets.long()] * (64.0 * 24 / H))[rows]
     d_ent = torch.randn(T, generator=g).to(DEV)
-    p = U.HeadParams(T=T, H=H, V=V, dtype="f32", kernel_path=path)
-    ws = U.alloc_head_workspace(p, DEV)
-    out = U.token_scores(p, hidden, W, targets, workspace=ws)
-    d_h, d_W = U.token_scores_bwd(p, hidden, W, None, out, None, d_ent, workspace=ws)
+    p, q = (U.HeadParams(T=T, H=H, V=V, dtype="f32", kernel_path=x) for x in (path.split("-")[0], path.split("-")[-1]))
+    out = U.token_scores(p, hidden, W, targets)
+    d_h, d_W = U.token_scores_bwd(q, hidden, W, None, out, None, d_ent)
     z = R.logits64(hidden, W, 1.0)
     dz, size = R.scores_dz64(z, targets, 1.0, None, d_ent)
     assert float(R.scores64(z, targets)["entropy"].min()) < 1e-5
