@@ -398,7 +398,8 @@ int ulorl_token_scores(const ulorl_head_params_t* params, const void* hidden, co
  *   dz[t, v] = kappa (d_logp (1[v = y_t] - p_v) - d_entropy p_v (ln p_v + entropy)),
  *   d_hidden = dz W (params->dtype), d_W = dz^T hidden (params->dw_dtype, added into when params->dw_accumulate).
  * norm, logp and entropy are the outputs of ulorl_token_scores (logp and targets are read with d_logp, entropy with
- * d_entropy).  A row whose two gradients are zero adds nothing, whatever its softmax; its hidden state must be
+ * d_entropy), for bf16 operands and d_entropy of a call with the same kernel_path (a peaked row's gradient of the entropy is
+ * smaller than what two paths' logits differ by; float32 operands may mix them).  A row whose two gradients are zero adds nothing, whatever its softmax; its hidden state must be
  * finite all the same.
  */
 int ulorl_token_scores_bwd(const ulorl_head_params_t* params, const void* hidden, const void* W,
