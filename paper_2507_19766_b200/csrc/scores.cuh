@@ -270,7 +270,7 @@ __device__ __forceinline__ RowSums merge_lanes(float m, float s, float u, int n,
 // 256 lane maxima bounds the k-th largest entry of the slice from below, and entries at or above it sit in lanes whose
 // maximum is: only their few vectors are read again.
 // Bound by issue slots (about ten instructions an entry): 4096 rows of 151936 bf16 take 247 us, 5.0 TB/s of the 6.5 that a copy
-// does, and 294 us with 8 alternatives; one row of float32 takes 10 us, 257 rows of 32003 float16 with 20 alternatives 12.
+// does, and 300 us with 8 alternatives; one row of float32 takes 10 us, 257 rows of 32003 float16 with 20 alternatives 12.
 // kHeld (the self-test of the bounded waits): the copies are never issued, and a wait gives up after args.wait_limit cycles.
 template <typename T, bool kHeld = false>
 __global__ void __launch_bounds__(kRowThreads, 4)
